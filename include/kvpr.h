@@ -53,6 +53,7 @@ extern "C" {
 #define KVPR_E_STATE  -5   /* call not valid in the current state (e.g. rows unwritten) */
 
 #define KVPR_F16 1
+#define KVPR_F32 2   /* where an entry point takes a type: q of kvpr_paged_attention, logits of kvpr_verify_drafts */
 /* Flags or-ed into kvpr_model_desc.dtype: keep the host store group-wise 4-bit compressed
  * (Sec. 4.4 "KV Cache Compression").  KV_INT4 compresses the cache rows, X_INT4 the stored
  * activations; KVPR_STORE_INT4 sets both.  All arithmetic stays float16 / float32: activation rows
@@ -443,6 +444,95 @@ int kvpr_rope_token(const void* qk32_dev, const void* table_dev, int n_pos, int 
 size_t kvpr_int4_row_bytes(int cols);
 int kvpr_quant_int4(const void* src_dev, void* dst_dev, int64_t rows, int cols, void* stream);
 int kvpr_dequant_int4(const void* src_dev, void* dst_dev, int64_t rows, int cols, void* stream);
+
+/* ---- ragged batches over a paged 4-bit cache ----
+ * Requests of different lengths on one GPU whose cache is held in 4 bits, in pages of a common pool, several new tokens per
+ * request and step: drafts to verify, prompt chunks, or one token each.  A step is
+ *     kvpr_paged_plan       pages, row offsets, slots and positions of the new tokens, from the lengths
+ *     kvpr_paged_append     per layer: rotate, pack the new tokens' k and v into their slots
+ *     kvpr_paged_attention  per layer: the new tokens over the pages
+ *     kvpr_verify_drafts    which drafts stand, the token behind them, and the lengths that the next plan starts from
+ * Lengths, tables and decisions stay on the device: no call waits, allocates or reads device memory from the host, so a step can be captured into a
+ * graph.  All arrays are device arrays, and calls that share written arrays or a workspace must run one after the
+ * other.  Arrays of one call must not overlap unless the text allows it.
+ *
+ * Rows.  The new tokens of all requests lie one behind the other: request r has rows row_start[r] .. row_start[r+1] - 1.  Every
+ * row-wise call takes n_rows, the rows its arrays have; rows behind row_start[n_requests] are left as they were, and no
+ * access goes past n_rows whatever row_start holds.
+ * Slots.  Position p of a request lies at slot = page * page_size + p % page_size, page = block_table[r][p / page_size].
+ * Pages.  The pool is n_pages * kvpr_page_bytes bytes, 16-byte aligned.  The values are those of kvpr_quant_int4 (groups of 64 columns of
+ * one head, (scale, minimum) in float16).  A page holds, for each key/value head, page_size * 9 * head_dim / 8 bytes:
+ *     key codes    [page_size][head_dim / 2]: the row's 4-byte words (8 columns each), word 4 s + g at place g (head_dim / 32) + s
+ *     value codes  [page_size / 4][head_dim / 2][4]: the bytes of four positions side by side, byte 32 u + 2 m + w of a row at
+ *                  place m (head_dim / 32) + 2 u + w
+ *     key pairs    [page_size][head_dim / 64] of (scale, minimum), then the value pairs likewise
+ * with column 2 k in the low four bits of byte k, column 2 k + 1 in the high ones. */
+typedef struct {
+    int32_t n_heads;       /* query heads; query head i reads key/value head i / (n_heads / n_kv_heads) */
+    int32_t n_kv_heads;    /* divides n_heads                                                   */
+    int32_t head_dim;      /* 64 or 128                                                         */
+    int32_t page_size;     /* positions per page: 16, 32, 64, 128 or 256                        */
+    int32_t n_pages;       /* pages in the pool; n_pages * page_size < 2^31                     */
+    int32_t table_width;   /* entries per request in block_table; table_width * page_size < 2^31 */
+} kvpr_paged_desc;
+
+size_t kvpr_page_bytes(const kvpr_paged_desc* desc);   /* 0 for a description that the calls refuse */
+
+/* The plan of one step.  base_len[r] positions of request r stay, new_len[r] tokens come (negative counts as 0): want = base_len + new_len,
+ * need = ceil(want / page_size) pages; held_in[r] it has, entries [0, held_in[r]) of its row of block_table [n_requests, table_width].
+ *  - Requests that hold more than they need (shorter, or finished: base_len = new_len = 0) give entries [need, held) back: pushed
+ *    onto the stack free_pages [n_pages] behind its free_count_in[0] entries, requests in order, entries in order.
+ *  - Then requests that need more take pages off the top, requests in order, into entries [held, need).  From the first that does not
+ *    find enough, requests that need pages are refused, and so is one whose need exceeds table_width (it takes none).
+ * Out: held_out[r] (need; held_in for a refused request), seq_len[r] = want (0 if refused), row_start [n_requests + 1] (sums of new_len),
+ * free_count_out[0], refused[0] = refused requests, and for each row slots[] (-1 where the request is refused) and positions[];
+ * rows behind the last request get slot -1, position 0, up to max_rows.  Other entries of block_table and free_pages stay as they are.
+ * held_out may be held_in and free_count_out may be free_count_in.  1 to 8192 requests; max_rows may be 0. */
+int kvpr_paged_plan(const kvpr_paged_desc* desc, const int32_t* base_len, const int32_t* new_len, int n_requests, int32_t* block_table,
+                    const int32_t* held_in, int32_t* held_out, int32_t* free_pages, const int32_t* free_count_in, int32_t* free_count_out,
+                    int max_rows, int32_t* row_start, int32_t* seq_len, int32_t* slots, int32_t* positions, int32_t* refused, void* stream);
+
+/* New tokens into the cache.  qkv float16 [n_rows] with row stride ld: [q (n_heads) | k (n_kv_heads) | v (n_kv_heads)] * head_dim columns, as one
+ * kvpr_token_gemm or kvpr_recompute_gemm gives them.  k and v of a row are packed into its slot; a slot outside the pool (-1 of the plan) stores nothing.
+ * With rope_table (device copy of kvpr_rope_table's [n_pos, head_dim/2, 2]) k is rotated first, and q rotated into q_out (float16, row
+ * stride ldq; null: not wanted; q itself, with ldq = ld, is allowed), both by the row's position, evaluated in 64 bits and rounded to
+ * float16 once; a row whose position lies outside [0, n_pos) is left out.  Without rope_table positions may be null and q_out must be.
+ * ld, ldq % 8 == 0; qkv, q_out, pages 16-byte aligned.  Two rows must not name the same slot. */
+int kvpr_paged_append(const kvpr_paged_desc* desc, const void* qkv, int64_t ld, const int32_t* slots, const int32_t* positions, int n_rows,
+                      const void* rope_table, int n_pos, void* q_out, int64_t ldq, void* pages, void* stream);
+/* Slots back to float16: row i of kv (row stride ld, ld % 8 == 0) = [k | v] of slots[i] as kvpr_dequant_int4 gives them.  Rows of slots
+ * outside the pool stay as they were. */
+int kvpr_paged_read(const kvpr_paged_desc* desc, const void* pages, const int32_t* slots, int n_rows, void* kv, int64_t ld, void* stream);
+
+/* Attention (Eq. 2) of the new tokens.  With m = row_start[r+1] - row_start[r] rows and seq_len[r] positions (the new tokens' own
+ * included), row i of request r sees positions [0, seq_len[r] - m + i + 1): z = softmax(q k^T / sqrt(head_dim)) v in float16, row stride ldz.
+ * A row that sees nothing gives 0.  k and v are code * scale + minimum without kvpr_dequant_int4's last rounding.  Positions whose table entry lies
+ * outside the pool, or behind table_width entries, take no part.
+ * q: KVPR_F16 or KVPR_F32, row stride ldq (elements).  max_new and max_len: how many new tokens and positions a request has at most,
+ * as far as the host knows; they size the launch and the workspace, and results are right for requests beyond them too.
+ * ldq, ldz % 8 == 0; q, pages, z, ws 16-byte aligned; ws needs kvpr_paged_attention_workspace_bytes of the same arguments. */
+size_t kvpr_paged_attention_workspace_bytes(const kvpr_paged_desc* desc, int n_requests, int n_rows, int max_new, int max_len);
+int kvpr_paged_attention(const kvpr_paged_desc* desc, const void* q, int q_type, int64_t ldq, const void* pages, const int32_t* block_table,
+                         const int32_t* row_start, const int32_t* seq_len, int n_requests, int n_rows, int max_new, int max_len, void* z,
+                         int64_t ldz, void* ws, size_t ws_bytes, void* stream);
+
+/* Verification of drafts.  Row 0 of a request is its last certain token, rows 1 .. m - 1 are drafts; tokens[] holds what was fed, target_logits
+ * [n_rows, vocab] (KVPR_F16 or KVPR_F32, row strides in elements) what the target model says after each row, draft_logits the distribution that the draft
+ * in the SAME row was drawn from (row 0's is not read); null: the drafts come without probabilities (a lookup), q = 1 at the draft.
+ *   p = softmax(target row i / T), q = softmax(draft row i + 1 / T), T = temperature[r];
+ *   draft x = tokens[row i + 1] stands if u_accept[row i + 1] q(x) < p(x); the first that does not ends the run;
+ *   the next token is the first v with sum_{w <= v} s(w) > u_sample[r] sum_w s(w), s = max(p - q, 0) of the row that was rejected (p where that
+ *   leaves nothing), s = p behind the last draft.  Shares and sums are evaluated in 64 bits.  u in [0, 1).
+ * T <= 0 (or NaN): greedy, a draft stands if it is the row's largest logit (lowest index on ties), and the next token is the largest one.
+ * Out: out_tokens of a request's rows: the drafts that stand, the next token, -1 for the rest; kept[r] = rows of the cache that stay = tokens gained
+ * (0 for a request without rows); len_out[r] = len_in[r] + kept[r] (both null: not wanted; the same array is allowed): with len_in = base_len, the next plan's base_len.
+ * A logit of NaN counts as -inf.  A target row of nothing but -inf has no distribution: the run ends there, and the next token is -1.  A draft outside
+ * [0, vocab) does not stand.  ws: 16-byte aligned, kvpr_verify_workspace_bytes bytes.  vocab at most 2^24. */
+size_t kvpr_verify_workspace_bytes(int n_requests, int n_rows, int vocab);
+int kvpr_verify_drafts(const void* target_logits, const void* draft_logits, int logits_type, int64_t ld_target, int64_t ld_draft, int vocab,
+                       const int32_t* tokens, const int32_t* row_start, int n_requests, int n_rows, const float* temperature,
+                       const float* u_accept, const float* u_sample, const int32_t* len_in, int32_t* len_out, int32_t* kept,
+                       int32_t* out_tokens, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libkvpr.so")
 
 KVPR_OK, KVPR_E_INVAL, KVPR_E_RANGE, KVPR_E_NOMEM, KVPR_E_HIP, KVPR_E_STATE = 0, -1, -2, -3, -4, -5
-KVPR_F16 = 1
+KVPR_F16, KVPR_F32 = 1, 2
 KVPR_KV_INT4, KVPR_X_INT4, KVPR_STORE_INT4 = 0x100, 0x200, 0x300
 KVPR_COST_EQ10, KVPR_COST_NS, KVPR_COST_ROW, KVPR_COST_PIPE = 0, 1, 2, 3
 KVPR_DEBUG_SYNC, KVPR_DEBUG_POISON = 1, 2
@@ -51,6 +51,10 @@ class kvpr_layer_timing(C.Structure):
 
     def as_dict(self):
         return {n: getattr(self, n) for n, _ in self._fields_}
+
+
+class kvpr_paged_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "table_width")]
 
 
 class KvprError(RuntimeError):
@@ -111,6 +115,14 @@ _SIGS = {
     "kvpr_int4_row_bytes": (_sz, [_i]),
     "kvpr_quant_int4": (_i, [_vp, _vp, _i64, _i, _vp]),
     "kvpr_dequant_int4": (_i, [_vp, _vp, _i64, _i, _vp]),
+    "kvpr_page_bytes": (_sz, [_vp]),
+    "kvpr_paged_plan": (_i, [_vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "kvpr_paged_append": (_i, [_vp, _vp, _i64, _vp, _vp, _i, _vp, _i, _vp, _i64, _vp, _vp]),
+    "kvpr_paged_read": (_i, [_vp, _vp, _vp, _i, _vp, _i64, _vp]),
+    "kvpr_paged_attention_workspace_bytes": (_sz, [_vp, _i, _i, _i, _i]),
+    "kvpr_paged_attention": (_i, [_vp, _vp, _i, _i64, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _i64, _vp, _sz, _vp]),
+    "kvpr_verify_workspace_bytes": (_sz, [_i, _i, _i]),
+    "kvpr_verify_drafts": (_i, [_vp, _vp, _i, _i64, _i64, _i, _vp, _vp, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
 }
 EXPORTS = tuple(_SIGS)
 for _name, (_res, _args) in _SIGS.items():
@@ -390,3 +402,84 @@ def kvpr_get_profile(ctx) -> kvpr_profile_t:
 def kvpr_decode_attention_mixed(q_dev, kv16_dev, kvq_dev, z_dev, ws_dev, S, split, batch, hidden, n_heads, stream=None):
     _check(lib.kvpr_decode_attention_mixed(_ptr(q_dev), _ptr(kv16_dev), _ptr(kvq_dev), _ptr(z_dev), _ptr(ws_dev), S, split,
                                            batch, hidden, n_heads, _stream(stream)))
+
+
+# ---- ragged batches over a paged 4-bit cache ----
+# Device arguments are checked to be tensors of the stated type on the current device: a host address in a kernel's hands
+# would end the process.
+
+_I32, _F16, _F32 = (torch.int32,), (torch.float16,), (torch.float32,)
+_LOGITS = {KVPR_F16: _F16, KVPR_F32: _F32}
+
+
+def _gpu(t, dtypes, name, device):
+    if t is None:
+        return None
+    if isinstance(t, int):
+        return t
+    if not t.is_cuda or t.get_device() != device:
+        raise ValueError(f"{name} must be on the current device cuda:{device}, got {t.device}")
+    if dtypes is not None and t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    return t.data_ptr()
+
+
+def make_paged_desc(n_heads, n_kv_heads, head_dim, page_size, n_pages, table_width) -> kvpr_paged_desc:
+    return kvpr_paged_desc(n_heads, n_kv_heads, head_dim, page_size, n_pages, table_width)
+
+
+def kvpr_page_bytes(desc) -> int:
+    return lib.kvpr_page_bytes(C.byref(desc))
+
+
+def kvpr_paged_plan(desc, base_len, new_len, n_requests, block_table, held_in, held_out, free_pages, free_count_in, free_count_out,
+                    max_rows, row_start, seq_len, slots, positions, refused, stream=None):
+    d = torch.cuda.current_device()
+    _check(lib.kvpr_paged_plan(C.byref(desc), _gpu(base_len, _I32, "base_len", d), _gpu(new_len, _I32, "new_len", d), n_requests,
+                               _gpu(block_table, _I32, "block_table", d), _gpu(held_in, _I32, "held_in", d), _gpu(held_out, _I32, "held_out", d),
+                               _gpu(free_pages, _I32, "free_pages", d), _gpu(free_count_in, _I32, "free_count_in", d),
+                               _gpu(free_count_out, _I32, "free_count_out", d), max_rows, _gpu(row_start, _I32, "row_start", d),
+                               _gpu(seq_len, _I32, "seq_len", d), _gpu(slots, _I32, "slots", d), _gpu(positions, _I32, "positions", d),
+                               _gpu(refused, _I32, "refused", d), _stream(stream)))
+
+
+def kvpr_paged_append(desc, qkv_dev, ld, slots, positions, n_rows, rope_table, n_pos, q_out, ldq, pages, stream=None):
+    d = torch.cuda.current_device()
+    _check(lib.kvpr_paged_append(C.byref(desc), _gpu(qkv_dev, _F16, "qkv_dev", d), ld, _gpu(slots, _I32, "slots", d),
+                                 _gpu(positions, _I32, "positions", d), n_rows, _gpu(rope_table, _F32, "rope_table", d), n_pos,
+                                 _gpu(q_out, _F16, "q_out", d), ldq, _gpu(pages, None, "pages", d), _stream(stream)))
+
+
+def kvpr_paged_read(desc, pages, slots, n_rows, kv_dev, ld, stream=None):
+    d = torch.cuda.current_device()
+    _check(lib.kvpr_paged_read(C.byref(desc), _gpu(pages, None, "pages", d), _gpu(slots, _I32, "slots", d), n_rows,
+                               _gpu(kv_dev, _F16, "kv_dev", d), ld, _stream(stream)))
+
+
+def kvpr_paged_attention_workspace_bytes(desc, n_requests, n_rows, max_new, max_len) -> int:
+    return lib.kvpr_paged_attention_workspace_bytes(C.byref(desc), n_requests, n_rows, max_new, max_len)
+
+
+def kvpr_paged_attention(desc, q_dev, q_type, ldq, pages, block_table, row_start, seq_len, n_requests, n_rows, max_new, max_len, z_dev, ldz,
+                         ws_dev, ws_bytes, stream=None):
+    d = torch.cuda.current_device()
+    _check(lib.kvpr_paged_attention(C.byref(desc), _gpu(q_dev, _LOGITS.get(q_type), "q_dev", d), q_type, ldq, _gpu(pages, None, "pages", d),
+                                    _gpu(block_table, _I32, "block_table", d), _gpu(row_start, _I32, "row_start", d),
+                                    _gpu(seq_len, _I32, "seq_len", d), n_requests, n_rows, max_new, max_len, _gpu(z_dev, _F16, "z_dev", d), ldz,
+                                    _gpu(ws_dev, None, "ws_dev", d), ws_bytes, _stream(stream)))
+
+
+def kvpr_verify_workspace_bytes(n_requests, n_rows, vocab) -> int:
+    return lib.kvpr_verify_workspace_bytes(n_requests, n_rows, vocab)
+
+
+def kvpr_verify_drafts(target_logits, draft_logits, logits_type, ld_target, ld_draft, vocab, tokens, row_start, n_requests, n_rows, temperature,
+                       u_accept, u_sample, len_in, len_out, kept, out_tokens, ws_dev, ws_bytes, stream=None):
+    d = torch.cuda.current_device()
+    types = _LOGITS.get(logits_type)
+    _check(lib.kvpr_verify_drafts(_gpu(target_logits, types, "target_logits", d), _gpu(draft_logits, types, "draft_logits", d), logits_type,
+                                  ld_target, ld_draft, vocab, _gpu(tokens, _I32, "tokens", d), _gpu(row_start, _I32, "row_start", d), n_requests,
+                                  n_rows, _gpu(temperature, _F32, "temperature", d), _gpu(u_accept, _F32, "u_accept", d),
+                                  _gpu(u_sample, _F32, "u_sample", d), _gpu(len_in, _I32, "len_in", d), _gpu(len_out, _I32, "len_out", d),
+                                  _gpu(kept, _I32, "kept", d), _gpu(out_tokens, _I32, "out_tokens", d), _gpu(ws_dev, None, "ws_dev", d), ws_bytes,
+                                  _stream(stream)))
