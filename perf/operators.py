@@ -479,7 +479,7 @@ def _own(st, case):
         kv.kvpr_paged_attention(st["desc"], st["q"], kv.KVPR_F16 if case["q"] == "f16" else kv.KVPR_F32, width, st["pages"], st["table"], st["row_start"],
                                 st["seq_len"], case["n"], st["rows"], max(st["new_host"]), max(st["lens"]), st["z"], width, st["ws"], st["ws"].numel())
         return st["z"]
-    kv.kvpr_verify_drafts(st["target"], st.get("draft"), kv.KVPR_F16 if case["type"] == "f16" else kv.KVPR_F32, case["vocab"], case["vocab"], st["tokens"],
+    kv.kvpr_verify_drafts(st["target"], st.get("draft"), kv.KVPR_F16 if case["type"] == "f16" else kv.KVPR_F32, case["vocab"], case["vocab"], case["vocab"], st["tokens"],
                           st["row_start"], case["n"], st["rows"], st["temperature"], st["u_accept"], st["u_sample"], st["len_in"], st["len_out"], st["kept"],
                           st["out"], st["ws"], st["ws"].numel())
     return {"tokens": st["out"], "kept": st["kept"], "len": st["len_out"]}
