@@ -506,7 +506,7 @@ int kvpr_paged_read(const kvpr_paged_desc* desc, const void* pages, const int32_
 
 /* Attention (Eq. 2) of the new tokens.  With m = row_start[r+1] - row_start[r] rows and seq_len[r] positions (the new tokens' own
  * included), row i of request r sees positions [0, seq_len[r] - m + i + 1): z = softmax(q k^T / sqrt(head_dim)) v in float16, row stride ldz.
- * A row that sees nothing gives 0.  k and v are code * scale + minimum without kvpr_dequant_int4's last rounding.  Positions whose table entry lies
+ * A row that sees nothing gives 0.  k is code * scale + minimum, v that rounded to float16 as kvpr_dequant_int4 gives it.  Positions whose table entry lies
  * outside the pool, or behind table_width entries, take no part.
  * q: KVPR_F16 or KVPR_F32, row stride ldq (elements).  max_new and max_len: how many new tokens and positions a request has at most,
  * as far as the host knows; they size the launch and the workspace, and results are right for requests beyond them too.

@@ -9,7 +9,8 @@ the library's order of work:
     kvpr_int4_oracle (groups of 64 columns of one head) into a page;
   * page: for each key/value head the bytes of `key codes | value codes | key pairs | value pairs`; words of 4 bytes of a key row in the order
     [g][s] of columns 8 (4 s + g); value bytes of four positions side by side, byte 32 u + 2 m + w of a row at place [m][u][w];
-  * attention: softmax(q k^T / sqrt(d)) v over the positions that a row sees, query head i with key/value head i / group;
+  * attention: softmax(q k^T / sqrt(d)) v over the positions that a row sees, query head i with key/value head i / group; k as
+    code * scale + minimum, v rounded to float16;
   * verification: a draft x stands if u q(x) < p(x); behind the first that does not, the token at which the running sum of max(p - q, 0)
     passes u times its total.
 """
@@ -148,9 +149,8 @@ def attention(q, pages, table, row_start, seq_len, heads, kv_heads, d, page, n_r
             for h in range(heads):
                 g = h // group
                 k = np.stack([values(*(a[g] for a in cache[j][0])) for j in see])
-                v = np.stack([values(*(a[g] for a in cache[j][1])) for j in see])
+                v = np.stack([values(*(a[g] for a in cache[j][1])) for j in see]).astype(np.float16).astype(np.float64)
                 ks = np.stack([np.repeat(15 * cache[j][0][1][g].astype(np.float64) + np.abs(cache[j][0][2][g].astype(np.float64)), io.GROUP) for j in see])
-                vs = np.stack([np.repeat(cache[j][1][1][g].astype(np.float64), io.GROUP) for j in see])
                 x = q[row, h * d:(h + 1) * d].astype(np.float64)
                 s = k @ x / np.sqrt(d)
                 p = np.exp(s - s.max())
@@ -158,7 +158,7 @@ def attention(q, pages, table, row_start, seq_len, heads, kv_heads, d, page, n_r
                 z[row, h] = p @ v
                 # a score passes about 16 roundings of 2^-24 of sums of |q| (15 scale + |minimum|); so do a weight and the sum of weights
                 off = 16 * 2.0 ** -24 * ((ks @ np.abs(x) / np.sqrt(d)).max() + 1)
-                tol[row, h] = 2.0 ** -11 * (p @ vs * 7.5 + np.abs(z[row, h])) + 2 * off * (p @ np.abs(v)) + 2.0 ** -25
+                tol[row, h] = 2.0 ** -11 * (p @ np.abs(v) + np.abs(z[row, h])) + 2 * off * (p @ np.abs(v)) + 2.0 ** -25
     return z.reshape(n_rows, -1), tol.reshape(n_rows, -1), done
 
 

@@ -1,101 +1,531 @@
 // Attention of a ragged batch's new tokens over a paged 4-bit cache (formulas at kvpr_paged_attention).
 //
-// One wave per (query head, new token): 64 positions at a time, a lane scores one position, then owns d / 64 columns of the sum.
+// The rows that share a key/value head - the new tokens times the query heads of its group - are the columns of the matrix
+// products, 16 a tile: scores^T = K q^T with the positions as rows of K, then z^T = V^T p^T.  A lane then holds four positions'
+// scores of one row (D fragment: column = lane & 15, rows 4 (lane >> 4) + 0..3), which are just the k values that it has to bring to the
+// second product, so that the weights never leave its registers.  32 positions a turn and wave:
+//   - a key lane (position lane & 15, g = lane >> 4) has one 16-byte load (d = 128) with its words of all steps, a value lane one
+//     with four positions of the columns that it sums: the order of the bytes in a page is made for this (paged.h);
+//   - a key's code as bits 0 - 3 (4 - 7) of a half is the subnormal number code 2^-24 (2^-20), which the matrix instruction takes
+//     exactly: unpacking is a mask.  The factor 16 of the odd columns is taken out of q; the affine map is taken out of the
+//     sum, k . q = scale (code . q) + minimum sum(q), per group of 64 columns, in float32;
+//   - values are unpacked to float16, as kvpr_dequant_int4 gives them: (1024 + code) - 1024 exactly, then one fused
+//     multiplication and addition;
+//   - q is scaled by a power of two per row to a largest element of 2^10 .. 2^11; float32 q is brought as the sum of two
+//     float16 numbers (the rest below 2^-22 of the largest element);
+//   - weights are 2^(score - ref) in float16 for the product, in float32 for their sum.  ref is the largest score less 6 when it was
+//     last set and is set again only when a weight would pass 2^15: no reduction over lanes in the usual turn, and
+//     weights keep all bits down to 2^-20 of the largest, some to 2^-30.
+// Work is split over key/value heads, requests, tiles of rows and chunks of positions; inside a workgroup the waves take turns of 32
+// positions (few rows) or rows of their own (many rows).  Partial sums of a request of several chunks meet in the workspace.
 #include "paged.h"
 #include <math.h>
+#include <algorithm>
 
 namespace kvpr {
 namespace {
 
-template <int D, class Q>
-__global__ __launch_bounds__(64) void paged_attention_kernel(PagedShape s, const Q* __restrict__ q, int64_t ldq, const uint8_t* __restrict__ pages,
-                                                             const int32_t* __restrict__ table, const int32_t* __restrict__ row_start,
-                                                             const int32_t* __restrict__ seq_len, int rows, _Float16* __restrict__ z,
-                                                             int64_t ldz, float scale_log2) {
-    constexpr int E = D / 64;
-    const int lane = threadIdx.x, head = blockIdx.x, r = blockIdx.y, kv_head = head / (s.heads / s.kv_heads);
-    const int first = row_start[r], m = row_start[r + 1] - first;
-    const int len = min(max(seq_len[r], 0), s.width * s.page);
-    __shared__ float qs[D], ps[64];
-    for (int i = blockIdx.z; i < m; i += gridDim.z) {
-        const int row = first + i;
-        if (row < 0 || row >= rows) break;
-        const int seen = min(len, seq_len[r] - m + i + 1);
-        __syncthreads();
-        for (int e = 0; e < E; ++e) qs[lane + 64 * e] = (float)q[row * ldq + (int64_t)head * D + lane + 64 * e];
-        __syncthreads();
-        float m_run = -0x1p126f, l_run = 0.f, acc[E] = {};     // finite, so that no difference of maxima is NaN
-        for (int t0 = 0; t0 < seen; t0 += 64) {
-            auto block_of = [&](int t) -> const uint8_t* {
-                const int id = table[(int64_t)r * s.width + (t >> s.page_log2)];
-                return id >= 0 && id < s.n_pages ? pages + id * s.page_bytes() + kv_head * s.block_bytes() : nullptr;
-            };
-            const int t = t0 + lane;
-            float score = -INFINITY;
-            const uint8_t* block = t < seen ? block_of(t) : nullptr;
-            if (block) {
-                const int u = t & (s.page - 1);
-                score = 0.f;
-                for (int g = 0; g < E; ++g) {
-                    const _Float16* meta = reinterpret_cast<const _Float16*>(block + s.page * D + (u * E + g) * 4);
-                    float dot = 0.f, sum = 0.f;
-                    for (int k = 0; k < 32; ++k) {
-                        const int byte = block[u * (D / 2) + key_place<D>(32 * g + k)];
-                        const float a = qs[64 * g + 2 * k], b = qs[64 * g + 2 * k + 1];
-                        dot += a * (float)(byte & 15) + b * (float)(byte >> 4);
-                        sum += a + b;
-                    }
-                    score += dot * (float)meta[0] + sum * (float)meta[1];
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+
+constexpr float LOWEST = -0x1p126f;     // where a reference starts: finite, so that no difference of two is NaN
+constexpr int TURN = 32;                // positions a wave takes at once
+
+// v of lanes l, l ^ 16, l ^ 32, l ^ 48 reduced; every lane gets the result
+template <class F>
+__device__ __forceinline__ float across_rows(float v, F f) {
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
+
+union Half8 {
+    half8 v;
+    uint32_t w[4];
+    half2v h[4];
+};
+
+struct AttentionArgs {
+    PagedShape s;
+    const void* q;
+    const uint8_t* pages;
+    const int32_t *table, *row_start, *seq_len;
+    _Float16* z;
+    float *acc, *ml;                    // partial sums [split][row * heads + head][d], (reference, sum of weights) likewise
+    int64_t ldq, ldz;
+    int rows, group, chunk, row_tiles;
+    float scale_log2;
+};
+
+// what the chunks of a request are, for the kernels on both sides of the workspace
+__device__ __forceinline__ int span_of(const AttentionArgs& a, int r) { return min(max(a.seq_len[r], 0), a.s.width * a.s.page); }
+
+// one turn's operands
+template <int D>
+struct Turn {
+    static constexpr int NG = D / 64, W = D / 32;
+    uint32_t k[2][W], v[2][W];
+    word4 km[2][NG], vm[2][NG];          // (scale, minimum) of four positions and NG groups
+};
+
+template <int D, int MT, bool F32, int NW, bool ROWS>
+__global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const AttentionArgs a) {
+    constexpr int NG = D / 64, W = D / 32, NT = 2 * W;   // groups, words of codes a lane has per 16 positions, tiles of 16 columns
+    const PagedShape& s = a.s;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m16 = lane & 15, g = lane >> 4;
+    const int kv_head = blockIdx.x % s.kv_heads, tile0 = blockIdx.x / s.kv_heads, r = blockIdx.y;
+    const int first = a.row_start[r], m = a.row_start[r + 1] - first, len = a.seq_len[r], span = span_of(a, r);
+    const int chunks = max((span + a.chunk - 1) / a.chunk, 1);
+    const int c0 = blockIdx.z * a.chunk, c1 = blockIdx.z == gridDim.z - 1 ? span : min(span, c0 + a.chunk);
+    if (c0 > 0 && c0 >= span) return;                                   // chunk 0 is there for empty requests too
+    const int64_t all_rows = (int64_t)m * a.group;
+    const int32_t* ids = a.table + (int64_t)r * s.width;
+    const int64_t page_bytes = s.page_bytes();
+    const uint8_t* head_base = a.pages + (int64_t)kv_head * s.block_bytes();
+    constexpr int TILE_ROWS = MT * 16 * (ROWS ? NW : 1);
+
+    for (int64_t row0 = (int64_t)tile0 * TILE_ROWS; row0 < all_rows; row0 += (int64_t)a.row_tiles * TILE_ROWS) {
+        const int64_t wave_row0 = row0 + (ROWS ? wave * MT * 16 : 0);
+        if (first + row0 / a.group >= a.rows) return;
+        // ---- rows: where they are, how far they see, q ----
+        int token[MT], head[MT], seen[MT];
+        bool real[MT];
+        Half8 q[MT][W], ql[F32 ? MT : 1][W];
+        float qs[MT][NG], to_log2[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int64_t rr = wave_row0 + mt * 16 + m16;
+            const int i = (int)(min(rr, all_rows - 1) / a.group);
+            token[mt] = first + i;
+            head[mt] = kv_head * a.group + (int)(min(rr, all_rows - 1) - (int64_t)i * a.group);
+            real[mt] = rr < all_rows && token[mt] >= 0 && token[mt] < a.rows;
+            seen[mt] = real[mt] ? min(span, len - m + i + 1) : 0;
+            const int64_t at = real[mt] ? token[mt] * a.ldq + (int64_t)head[mt] * D : 0;
+            float x[W][8], big = 0.f;
+#pragma unroll
+            for (int st = 0; st < W; ++st) {
+                const int col = (st * 4 + g) * 8;
+                if constexpr (F32) {
+                    const float4v* p = reinterpret_cast<const float4v*>((const float*)a.q + at + col);
+                    const float4v u = p[0], w = p[1];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { x[st][e] = u[e]; x[st][4 + e] = w[e]; }
+                } else {
+                    const half8 u = *reinterpret_cast<const half8*>((const _Float16*)a.q + at + col);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[st][e] = (float)u[e];
                 }
-                score *= scale_log2;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(x[st][e]));
             }
-            float m_new = score;
-            for (int o = 32; o > 0; o >>= 1) m_new = fmaxf(m_new, __shfl_xor(m_new, o));
-            m_new = fmaxf(m_new, m_run);
-            const float p = exp2f(score - m_new), keep = exp2f(m_run - m_new);
-            float p_sum = p;
-            for (int o = 32; o > 0; o >>= 1) p_sum += __shfl_xor(p_sum, o);
-            l_run = l_run * keep + p_sum;
-            m_run = m_new;
-            ps[lane] = p;
-            __syncthreads();
-            for (int e = 0; e < E; ++e) acc[e] *= keep;
-            for (int j = 0; j < 64 && t0 + j < seen; ++j) {
-                const uint8_t* from = block_of(t0 + j);
-                if (!from) continue;
-                const int u = (t0 + j) & (s.page - 1);
-                for (int e = 0; e < E; ++e) {
-                    const int k = 32 * e + lane / 2;
-                    const int byte = from[s.page * (D / 2) + (u >> 2) * (2 * D) + value_place<D>(k) * 4 + (u & 3)];
-                    const _Float16* meta = reinterpret_cast<const _Float16*>(from + s.page * D + s.page * (D / 16) + (u * E + e) * 4);
-                    const int code = lane & 1 ? byte >> 4 : byte & 15;
-                    acc[e] += ps[j] * ((float)code * (float)meta[0] + (float)meta[1]);
+            big = across_rows(big, max_of);
+            // exponent of the largest element; of 0 and of infinite or NaN rows whatever
+            const int ex = min(max((int)(__float_as_uint(big) >> 23) - 127, -100), 100);
+            const float up = __uint_as_float((uint32_t)(127 + 10 - ex) << 23);
+            to_log2[mt] = a.scale_log2 * __uint_as_float((uint32_t)(127 + 24 - 10 + ex) << 23);
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                float t = 0.f;
+#pragma unroll
+                for (int st = 2 * gr; st < 2 * gr + 2; ++st)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) t += x[st][e] * up;
+                qs[mt][gr] = across_rows(t, sum_of) * 0x1p-24f;
+            }
+#pragma unroll
+            for (int st = 0; st < W; ++st) {
+                constexpr int order[8] = {0, 4, 1, 5, 2, 6, 3, 7};      // columns as the masks below leave them
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float y = x[st][order[e]] * up * ((e & 2) ? 0.0625f : 1.f);
+                    const _Float16 hi = (_Float16)y;
+                    q[mt][st].v[e] = hi;
+                    if constexpr (F32) ql[mt][st].v[e] = (_Float16)(y - (float)hi);
+                }
+            }
+        }
+        // positions that every / any row of the wave sees
+        int all_see = 0x7fffffff, any_see = 0;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            all_see = min(all_see, real[mt] ? seen[mt] : 0x7fffffff);
+            any_see = max(any_see, seen[mt]);
+        }
+        for (int o = 1; o < 16; o <<= 1) {
+            all_see = min(all_see, __shfl_xor(all_see, o));
+            any_see = max(any_see, __shfl_xor(any_see, o));
+        }
+        all_see = __builtin_amdgcn_readfirstlane(all_see);
+        any_see = __builtin_amdgcn_readfirstlane(any_see);
+        const int end = min(c1, any_see);
+
+        float ref[MT], l[MT];
+        float4v acc[MT][NT];
+        float spoilt[MT][NG];                                           // NaN once a row has seen values that are not finite in a masked turn
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            ref[mt] = LOWEST;
+            l[mt] = 0.f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[mt][t] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) spoilt[mt][gr] = 0.f;
+        }
+
+        auto id_of = [&](int t) { return t < end ? ids[t >> s.page_log2] : -1; };
+        auto load = [&](Turn<D>& x, int t0, const int (&id)[2]) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                // a turn's halves that lie behind the end or outside the pool read the pool's first page and are masked
+                const int t = t0 + 16 * u, tp = t & (s.page - 1);
+                const uint8_t* b = head_base + (int64_t)((unsigned)id[u] < (unsigned)s.n_pages ? id[u] : 0) * page_bytes;
+                const uint8_t* kp = b + (tp + m16) * (D / 2) + g * (D / 8);
+                const uint8_t* vp = b + s.page * (D / 2) + ((tp >> 2) + g) * (2 * D) + m16 * (D / 8);
+                const uint8_t* mp = b + s.page * D + (tp + 4 * g) * (NG * 4);
+                if constexpr (D == 128) {
+                    const word4 kw = *reinterpret_cast<const word4*>(kp), vw = *reinterpret_cast<const word4*>(vp);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) { x.k[u][i] = kw[i]; x.v[u][i] = vw[i]; }
+                } else {
+                    const uint2 kw = *reinterpret_cast<const uint2*>(kp), vw = *reinterpret_cast<const uint2*>(vp);
+                    x.k[u][0] = kw.x; x.k[u][1] = kw.y; x.v[u][0] = vw.x; x.v[u][1] = vw.y;
+                }
+#pragma unroll
+                for (int i = 0; i < NG; ++i) {
+                    x.km[u][i] = reinterpret_cast<const word4*>(mp)[i];
+                    x.vm[u][i] = reinterpret_cast<const word4*>(mp + s.page * (NG * 4))[i];
+                }
+            }
+        };
+        auto pair = [](const word4 (&w)[NG], int pos, int gr) {
+            half2v h;
+            const uint32_t v = w[(pos * NG + gr) >> 2][(pos * NG + gr) & 3];
+            __builtin_memcpy(&h, &v, 4);
+            return h;                                                   // (scale, minimum)
+        };
+        auto compute = [&](Turn<D>& x, int t0, const int (&id)[2]) {
+            const bool masked = t0 + TURN > all_see || t0 + TURN > c1 || (unsigned)id[0] >= (unsigned)s.n_pages || (unsigned)id[1] >= (unsigned)s.n_pages;
+            // ---- scores ----
+            float sc[MT][2][4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float4v c[MT][NG];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int gr = 0; gr < NG; ++gr) c[mt][gr] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int st = 0; st < W; ++st) {
+                    Half8 kf;
+                    const uint32_t w = x.k[u][st], w8 = w >> 8;
+                    kf.w[0] = w & 0x000F000Fu; kf.w[1] = w & 0x00F000F0u; kf.w[2] = w8 & 0x000F000Fu; kf.w[3] = w8 & 0x00F000F0u;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        c[mt][st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf.v, q[mt][st].v, c[mt][st / 2], 0, 0, 0);
+                        if constexpr (F32) c[mt][st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf.v, ql[mt][st].v, c[mt][st / 2], 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        float t = 0.f;
+#pragma unroll
+                        for (int gr = 0; gr < NG; ++gr) {
+                            const half2v sm = pair(x.km[u], p, gr);
+                            t = fmaf((float)sm[0], c[mt][gr][p], fmaf((float)sm[1], qs[mt][gr], t));
+                        }
+                        sc[mt][u][p] = t * to_log2[mt];
+                    }
+            }
+            if (masked) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const bool there = (unsigned)id[u] < (unsigned)s.n_pages;
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        const int t = t0 + 16 * u + 4 * g + p;
+                        bool finite[NG];
+#pragma unroll
+                        for (int gr = 0; gr < NG; ++gr) {
+                            const half2v sm = pair(x.vm[u], p, gr);
+                            finite[gr] = fabsf((float)sm[0]) < INFINITY && fabsf((float)sm[1]) < INFINITY;
+                            // positions that a row does not see must not reach its sum, not even as 0 times NaN
+                            if (!there || t >= end || !finite[gr]) x.vm[u][(p * NG + gr) >> 2][(p * NG + gr) & 3] = 0u;
+                        }
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            const bool sees = there && t < c1 && t < seen[mt];
+                            if (!sees) sc[mt][u][p] = -INFINITY;
+#pragma unroll
+                            for (int gr = 0; gr < NG; ++gr)
+                                if (sees && !finite[gr]) spoilt[mt][gr] = NAN;
+                        }
+                    }
+                }
+            }
+            // ---- weights ----
+            Half8 pw[MT];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                float top = sc[mt][0][0];
+#pragma unroll
+                for (int j = 1; j < 8; ++j) top = fmaxf(top, sc[mt][j >> 2][j & 3]);
+                if (__any(top - ref[mt] > 15.f)) {
+                    const float now = fmaxf(ref[mt], across_rows(top, max_of) - 6.f);
+                    const float keep = exp2f(ref[mt] - now);
+                    ref[mt] = now;
+                    l[mt] *= keep;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) acc[mt][t] *= keep;
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    float p[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        p[j] = __builtin_amdgcn_exp2f(sc[mt][u][j] - ref[mt]);
+                        l[mt] += p[j];
+                    }
+                    // order of the positions as the masks below leave them
+                    pw[mt].h[2 * u] = half2v{(_Float16)p[0], (_Float16)p[2]};
+                    pw[mt].h[2 * u + 1] = half2v{(_Float16)p[1], (_Float16)p[3]};
+                }
+            }
+            // ---- values ----
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                half2v sc2[2][2], mn2[2][2];                            // [half of the turn][positions 0, 2 | 1, 3]
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int o = 0; o < 2; ++o) {
+                        const half2v lo = pair(x.vm[u], o, gr), hi = pair(x.vm[u], o + 2, gr);
+                        sc2[u][o] = half2v{lo[0], hi[0]};
+                        mn2[u][o] = half2v{lo[1], hi[1]};
+                    }
+#pragma unroll
+                for (int i = 2 * gr; i < 2 * gr + 2; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        Half8 vf;
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int o = 0; o < 2; ++o) {
+                                const uint32_t w = o ? x.v[u][i] >> 8 : x.v[u][i];
+                                const uint32_t biased = h ? (w >> 4 & 0x000F000Fu) | 0x64006400u : (w & 0x000F000Fu) | 0x64006400u;
+                                half2v c;
+                                __builtin_memcpy(&c, &biased, 4);
+                                c -= half2v{(_Float16)1024.f, (_Float16)1024.f};
+                                vf.h[2 * u + o] = __builtin_elementwise_fma(c, sc2[u][o], mn2[u][o]);
+                            }
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt)
+                            acc[mt][2 * i + h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf.v, pw[mt].v, acc[mt][2 * i + h], 0, 0, 0);
+                    }
+            }
+        };
+
+        const int step = ROWS ? TURN : NW * TURN;
+        int t0 = c0 + (ROWS ? 0 : wave * TURN);
+        if (t0 < end) {
+            Turn<D> cur, nxt;
+            int id[2] = {id_of(t0), id_of(t0 + 16)}, id1[2] = {id_of(t0 + step), id_of(t0 + step + 16)};
+            load(cur, t0, id);
+            while (true) {
+                const int t1 = t0 + step;
+                int id2[2] = {id_of(t1 + step), id_of(t1 + step + 16)};
+                if (t1 < end) load(nxt, t1, id1);
+                compute(cur, t0, id);
+                if (t1 >= end) break;
+                cur = nxt;
+                t0 = t1;
+                id[0] = id1[0]; id[1] = id1[1];
+                id1[0] = id2[0]; id1[1] = id2[1];
+            }
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            l[mt] = across_rows(l[mt], sum_of);
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                const float bad = across_rows(spoilt[mt][gr], sum_of);
+#pragma unroll
+                for (int t = 4 * gr; t < 4 * gr + 4; ++t)
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) acc[mt][t][p] += bad;
+            }
+        }
+        // writes columns 64 gr + 16 g + 4 p .. + 3 of one row from what = acc over (w, h)
+        auto put = [&](int mt, int p, int gr, const float (&what)[4], float ref_, float l_) {
+            if (!real[mt]) return;
+            const int col = 64 * gr + (4 * g + p) * 4;
+            if (chunks == 1 || gridDim.z == 1) {
+                const float inv = l_ == 0.f ? 0.f : 1.f / l_;
+                half4 out;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[e] = (_Float16)(l_ == 0.f ? 0.f : what[e] * inv);
+                *reinterpret_cast<half4*>(a.z + token[mt] * a.ldz + (int64_t)head[mt] * D + col) = out;
+            } else {
+                const int64_t slot = ((int64_t)blockIdx.z * a.rows + token[mt]) * s.heads + head[mt];
+                *reinterpret_cast<float4v*>(a.acc + slot * D + col) = float4v{what[0], what[1], what[2], what[3]};
+                if (col == 0) *reinterpret_cast<float2*>(a.ml + slot * 2) = make_float2(ref_, l_);
+            }
+        };
+        if constexpr (ROWS) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int p = 0; p < 4; ++p)
+#pragma unroll
+                    for (int gr = 0; gr < NG; ++gr) {
+                        const float what[4] = {acc[mt][4 * gr][p], acc[mt][4 * gr + 1][p], acc[mt][4 * gr + 2][p], acc[mt][4 * gr + 3][p]};
+                        put(mt, p, gr, what, ref[mt], l[mt]);
+                    }
+        } else {
+            // the waves' sums meet in LDS, a tile of rows at a time; wave w then has the columns of p = w (and w + 4 ..)
+            __shared__ float part[NW][4][NT][64];
+            __shared__ float2 ml[NW][16];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                __syncthreads();
+                if (g == 0) ml[wave][m16] = make_float2(ref[mt], l[mt]);
+                __syncthreads();
+                float top = LOWEST, sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < NW; ++w) top = fmaxf(top, ml[w][m16].x);
+#pragma unroll
+                for (int w = 0; w < NW; ++w) sum += ml[w][m16].y * exp2f(ml[w][m16].x - top);
+                const float mine = exp2f(ref[mt] - top);
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) part[wave][p][t][lane] = acc[mt][t][p] * mine;
+                __syncthreads();
+                for (int j = wave; j < 4 * NG; j += NW) {
+                    const int p = j & 3, gr = j >> 2;
+                    float what[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int w = 0; w < NW; ++w)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) what[e] += part[w][p][4 * gr + e][lane];
+                    put(mt, p, gr, what, top, sum);
                 }
             }
             __syncthreads();
         }
-        for (int e = 0; e < E; ++e)
-            z[row * ldz + (int64_t)head * D + lane + 64 * e] = (_Float16)(l_run == 0.f ? 0.f : acc[e] / l_run);
     }
 }
 
+// Joins the chunks of requests that have several: one wave per (row, head).
+template <int D>
+__global__ __launch_bounds__(256) void paged_attention_join(const AttentionArgs a) {
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63, r = blockIdx.y;
+    const int span = span_of(a, r), chunks = min((span + a.chunk - 1) / a.chunk, a.row_tiles);   // row_tiles: chunks of the launch
+    if (chunks <= 1) return;
+    const int first = a.row_start[r];
+    const int64_t pairs = (int64_t)(a.row_start[r + 1] - first) * a.s.heads;
+    for (int64_t j = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); j < pairs; j += (int64_t)gridDim.x * 4) {
+        const int64_t token = first + j / a.s.heads, head = j % a.s.heads;
+        if (token < 0 || token >= a.rows) return;
+        const int64_t at = token * a.s.heads + head, stride = (int64_t)a.rows * a.s.heads;
+        float top = LOWEST, l = 0.f, o[E] = {};
+        for (int c = 0; c < chunks; ++c) top = fmaxf(top, a.ml[(c * stride + at) * 2]);
+        for (int c = 0; c < chunks; ++c) {
+            const float2 ml = *reinterpret_cast<const float2*>(a.ml + (c * stride + at) * 2);
+            const float w = exp2f(ml.x - top);
+            l += ml.y * w;
+            const float* p = a.acc + (c * stride + at) * D + lane * E;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] += p[e] * w;
+        }
+        _Float16* z = a.z + token * a.ldz + head * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[e] = (_Float16)(l == 0.f ? 0.f : o[e] / l);
+    }
+}
+
+// how a launch is cut
+struct Cut {
+    int mt;             // tiles of 16 rows a wave
+    bool rows;          // the waves of a workgroup have rows of their own
+    int row_tiles, chunk, chunks;
+};
+constexpr int NW = 4;
+
+Cut cut_of(const PagedShape& s, int n, int max_new, int max_len, bool) {
+    Cut c;
+    const int64_t r = (int64_t)max_new * (s.heads / s.kv_heads);
+    c.mt = r <= 16 ? 1 : 2;
+    c.rows = r > 128;
+    const int tile = c.mt * 16 * (c.rows ? NW : 1);
+    c.row_tiles = (int)std::min<int64_t>((r + tile - 1) / tile, 65535 / 8);
+    const int64_t len = std::min<int64_t>(max_len, (int64_t)s.width * s.page);
+    const int64_t units = (int64_t)n * s.kv_heads * c.row_tiles;
+    const int64_t want = std::max<int64_t>(1, 1024 / units), least = c.rows ? 512 : NW * TURN;
+    int64_t chunk = std::max(least, (len + want - 1) / want);
+    if (!c.rows) chunk = std::min<int64_t>(chunk, 2048);
+    chunk = (chunk + NW * TURN - 1) / (NW * TURN) * (NW * TURN);
+    chunk = std::max(chunk, (len + 1023) / 1024 / (NW * TURN) * (NW * TURN));     // at most about 1024 chunks
+    c.chunk = (int)std::min<int64_t>(chunk, 0x7fffffff / 2);
+    c.chunks = (int)std::max<int64_t>(1, (len + c.chunk - 1) / c.chunk);
+    return c;
+}
+
+int64_t part_floats(const PagedShape& s, int rows, const Cut& c) { return c.chunks > 1 ? (int64_t)c.chunks * rows * s.heads : 0; }
+
 }  // namespace
 
-size_t paged_attention_workspace_bytes(const PagedShape&, int, int, int, int) { return 16; }
+size_t paged_attention_workspace_bytes(const PagedShape& s, int n, int rows, int max_new, int max_len) {
+    return (size_t)part_floats(s, rows, cut_of(s, n, max_new, max_len, false)) * (s.d + 2) * 4 + 16;
+}
 
-int launch_paged_attention(const PagedShape& s, const PagedAttention& a, void*, size_t, hipStream_t st) {
-    const float scale_log2 = (float)(1.4426950408889634 / sqrt((double)s.d));
-    const dim3 grid((unsigned)s.heads, (unsigned)a.n, (unsigned)(a.max_new < 1024 ? a.max_new : 1024));
-#define KVPR_LAUNCH(D_, Q_)                                                                                                                   \
-    hipLaunchKernelGGL((paged_attention_kernel<D_, Q_>), grid, dim3(64), 0, st, s, (const Q_*)a.q, a.ldq, (const uint8_t*)a.pages, a.table,   \
-                       a.row_start, a.seq_len, a.rows, (_Float16*)a.z, a.ldz, scale_log2)
+int launch_paged_attention(const PagedShape& s, const PagedAttention& x, void* ws, size_t, hipStream_t st) {
+    const Cut c = cut_of(s, x.n, x.max_new, x.max_len, x.q_f32);
+    AttentionArgs a;
+    a.s = s;
+    a.q = x.q;
+    a.pages = (const uint8_t*)x.pages;
+    a.table = x.table; a.row_start = x.row_start; a.seq_len = x.seq_len;
+    a.z = (_Float16*)x.z;
+    a.acc = (float*)ws;
+    a.ml = a.acc + part_floats(s, x.rows, c) * s.d;
+    a.ldq = x.ldq; a.ldz = x.ldz;
+    a.rows = x.rows; a.group = s.heads / s.kv_heads; a.chunk = c.chunk; a.row_tiles = c.row_tiles;
+    a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)s.d));
+    const dim3 grid((unsigned)(s.kv_heads * c.row_tiles), (unsigned)x.n, (unsigned)c.chunks);
+#define KVPR_LAUNCH(D_, MT_, F32_, ROWS_) hipLaunchKernelGGL((paged_attention_kernel<D_, MT_, F32_, NW, ROWS_>), grid, dim3(NW * 64), 0, st, a)
+#define KVPR_BY_MT(D_, F32_)                                                      \
+    do {                                                                          \
+        if (c.rows) KVPR_LAUNCH(D_, 2, F32_, true);                               \
+        else if (c.mt == 1) KVPR_LAUNCH(D_, 1, F32_, false);                      \
+        else KVPR_LAUNCH(D_, 2, F32_, false);                                     \
+    } while (0)
     if (s.d == 128) {
-        if (a.q_f32) KVPR_LAUNCH(128, float); else KVPR_LAUNCH(128, _Float16);
+        if (x.q_f32) KVPR_BY_MT(128, true); else KVPR_BY_MT(128, false);
     } else {
-        if (a.q_f32) KVPR_LAUNCH(64, float); else KVPR_LAUNCH(64, _Float16);
+        if (x.q_f32) KVPR_BY_MT(64, true); else KVPR_BY_MT(64, false);
     }
+#undef KVPR_BY_MT
 #undef KVPR_LAUNCH
     KVPR_HIP(hipGetLastError());
+    if (c.chunks > 1) {
+        a.row_tiles = c.chunks;
+        const int64_t pairs = (int64_t)x.max_new * s.heads;
+        const dim3 joined((unsigned)std::min<int64_t>((pairs + 3) / 4, 4096), (unsigned)x.n);
+        if (s.d == 128) hipLaunchKernelGGL(paged_attention_join<128>, joined, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL(paged_attention_join<64>, joined, dim3(256), 0, st, a);
+        KVPR_HIP(hipGetLastError());
+    }
     return KVPR_OK;
 }
 
