@@ -13,7 +13,8 @@
 //     multiplication and addition;
 //   - q is scaled by a power of two per row to a largest element of 2^10 .. 2^11; float32 q is brought as the sum of two
 //     float16 numbers (the rest below 2^-22 of the largest element);
-//   - weights are 2^(score - ref) in float16 for the product, in float32 for their sum.  ref is the largest score less 6 when it was
+//   - weights are 2^(score - ref), brought to the product as the sum of two float16 numbers (one alone made the result's error 1.6
+//     times that of its own rounding), summed in float32.  ref is the largest score less 6 when it was
 //     last set and is set again only when a weight would pass 2^15: no reduction over lanes in the usual turn, and
 //     weights keep all bits down to 2^-20 of the largest, some to 2^-30.
 // Work is split over key/value heads, requests, tiles of rows and chunks of positions; inside a workgroup the waves take turns of 32
@@ -45,6 +46,12 @@ __device__ __forceinline__ float across_rows(float v, F f) {
 __device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
 
+// what a wave writes to LDS, its lanes read in program order
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 union Half8 {
     half8 v;
     uint32_t w[4];
@@ -66,12 +73,26 @@ struct AttentionArgs {
 // what the chunks of a request are, for the kernels on both sides of the workspace
 __device__ __forceinline__ int span_of(const AttentionArgs& a, int r) { return min(max(a.seq_len[r], 0), a.s.width * a.s.page); }
 
-// one turn's operands
+// One turn's operands as they are loaded: the codes, and of the (scale, minimum) pairs of the 32 positions' keys and values, 512
+// bytes, one lane's share.  The pairs go through LDS, where every lane reads those of its four positions: sixteen lanes
+// need the same ones, and loading them so from the pages took 8 of 12 loads and 64 of 96 registers for two turns.
 template <int D>
 struct Turn {
     static constexpr int NG = D / 64, W = D / 32;
-    uint32_t k[2][W], v[2][W];
-    word4 km[2][NG], vm[2][NG];          // (scale, minimum) of four positions and NG groups
+    uint32_t k[2][W], v[2][W], pairs[NG];
+};
+// (scale, minimum) of four positions and NG groups
+template <int D>
+struct Pairs {
+    static constexpr int NG = D / 64;
+    word4 w[NG];
+    __device__ half2v at(int pos, int gr) const {
+        half2v h;
+        const uint32_t v = w[(pos * NG + gr) >> 2][(pos * NG + gr) & 3];
+        __builtin_memcpy(&h, &v, 4);
+        return h;
+    }
+    __device__ void clear(int pos, int gr) { w[(pos * NG + gr) >> 2][(pos * NG + gr) & 3] = 0u; }
 };
 
 template <int D, int MT, bool F32, int NW, bool ROWS>
@@ -90,6 +111,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
     const int64_t page_bytes = s.page_bytes();
     const uint8_t* head_base = a.pages + (int64_t)kv_head * s.block_bytes();
     constexpr int TILE_ROWS = MT * 16 * (ROWS ? NW : 1);
+    __shared__ uint32_t pair_lds[NW][64 * NG];
 
     for (int64_t row0 = (int64_t)tile0 * TILE_ROWS; row0 < all_rows; row0 += (int64_t)a.row_tiles * TILE_ROWS) {
         const int64_t wave_row0 = row0 + (ROWS ? wave * MT * 16 : 0);
@@ -179,40 +201,49 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
             for (int gr = 0; gr < NG; ++gr) spoilt[mt][gr] = 0.f;
         }
 
+        const uint32_t k_lane = m16 * (D / 2) + g * (D / 8), v_lane = s.page * (D / 2) + g * (2 * D) + m16 * (D / 8),
+                       p_lane = s.page * D + (lane & 16 ? s.page * (NG * 4) : 0) + m16 * (NG * 4);
         auto id_of = [&](int t) { return t < end ? ids[t >> s.page_log2] : -1; };
         auto load = [&](Turn<D>& x, int t0, const int (&id)[2]) {
+            const uint8_t* pb[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 // a turn's halves that lie behind the end or outside the pool read the pool's first page and are masked
-                const int t = t0 + 16 * u, tp = t & (s.page - 1);
+                const int tp = (t0 + 16 * u) & (s.page - 1);
                 const uint8_t* b = head_base + (int64_t)((unsigned)id[u] < (unsigned)s.n_pages ? id[u] : 0) * page_bytes;
-                const uint8_t* kp = b + (tp + m16) * (D / 2) + g * (D / 8);
-                const uint8_t* vp = b + s.page * (D / 2) + ((tp >> 2) + g) * (2 * D) + m16 * (D / 8);
-                const uint8_t* mp = b + s.page * D + (tp + 4 * g) * (NG * 4);
+                pb[u] = b + tp * (NG * 4);
+                const uint8_t* cb = b + tp * (D / 2);
                 if constexpr (D == 128) {
-                    const word4 kw = *reinterpret_cast<const word4*>(kp), vw = *reinterpret_cast<const word4*>(vp);
+                    const word4 kw = *reinterpret_cast<const word4*>(cb + k_lane), vw = *reinterpret_cast<const word4*>(cb + v_lane);
 #pragma unroll
                     for (int i = 0; i < W; ++i) { x.k[u][i] = kw[i]; x.v[u][i] = vw[i]; }
                 } else {
-                    const uint2 kw = *reinterpret_cast<const uint2*>(kp), vw = *reinterpret_cast<const uint2*>(vp);
+                    const uint2 kw = *reinterpret_cast<const uint2*>(cb + k_lane), vw = *reinterpret_cast<const uint2*>(cb + v_lane);
                     x.k[u][0] = kw.x; x.k[u][1] = kw.y; x.v[u][0] = vw.x; x.v[u][1] = vw.y;
                 }
-#pragma unroll
-                for (int i = 0; i < NG; ++i) {
-                    x.km[u][i] = reinterpret_cast<const word4*>(mp)[i];
-                    x.vm[u][i] = reinterpret_cast<const word4*>(mp + s.page * (NG * 4))[i];
-                }
+            }
+            const uint32_t* pp = reinterpret_cast<const uint32_t*>((lane & 32 ? pb[1] : pb[0]) + p_lane);
+            if constexpr (D == 128) {
+                const uint2 w = *reinterpret_cast<const uint2*>(pp);
+                x.pairs[0] = w.x; x.pairs[1] = w.y;
+            } else {
+                x.pairs[0] = *pp;
             }
         };
-        auto pair = [](const word4 (&w)[NG], int pos, int gr) {
-            half2v h;
-            const uint32_t v = w[(pos * NG + gr) >> 2][(pos * NG + gr) & 3];
-            __builtin_memcpy(&h, &v, 4);
-            return h;                                                   // (scale, minimum)
-        };
-        auto compute = [&](Turn<D>& x, int t0, const int (&id)[2]) {
+        auto compute = [&](const Turn<D>& x, int t0, const int (&id)[2]) {
             const bool masked = t0 + TURN > all_see || t0 + TURN > c1 || (unsigned)id[0] >= (unsigned)s.n_pages || (unsigned)id[1] >= (unsigned)s.n_pages;
-            // ---- scores ----
+            uint32_t* mine = pair_lds[wave];
+            if constexpr (D == 128) *reinterpret_cast<uint2*>(mine + 2 * lane) = make_uint2(x.pairs[0], x.pairs[1]);
+            else mine[lane] = x.pairs[0];
+            wave_fence();
+            auto pairs_of = [&](int u, int values) {
+                Pairs<D> r;
+                const word4* from = reinterpret_cast<const word4*>(mine + ((u * 2 + values) * 16 + g * 4) * NG);
+#pragma unroll
+                for (int i = 0; i < NG; ++i) r.w[i] = from[i];
+                return r;
+            };
+            // ---- scores, in units of 2^to_log2 ----
             float sc[MT][2][4];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -232,6 +263,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
                         if constexpr (F32) c[mt][st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf.v, ql[mt][st].v, c[mt][st / 2], 0, 0, 0);
                     }
                 }
+                const Pairs<D> km = pairs_of(u, 0);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -239,12 +271,14 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
                         float t = 0.f;
 #pragma unroll
                         for (int gr = 0; gr < NG; ++gr) {
-                            const half2v sm = pair(x.km[u], p, gr);
+                            const half2v sm = km.at(p, gr);
                             t = fmaf((float)sm[0], c[mt][gr][p], fmaf((float)sm[1], qs[mt][gr], t));
                         }
-                        sc[mt][u][p] = t * to_log2[mt];
+                        sc[mt][u][p] = t;
                     }
             }
+            Pairs<D> vm[2] = {pairs_of(0, 1), pairs_of(1, 1)};
+            wave_fence();
             if (masked) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
@@ -255,10 +289,10 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
                         bool finite[NG];
 #pragma unroll
                         for (int gr = 0; gr < NG; ++gr) {
-                            const half2v sm = pair(x.vm[u], p, gr);
+                            const half2v sm = vm[u].at(p, gr);
                             finite[gr] = fabsf((float)sm[0]) < INFINITY && fabsf((float)sm[1]) < INFINITY;
                             // positions that a row does not see must not reach its sum, not even as 0 times NaN
-                            if (!there || t >= end || !finite[gr]) x.vm[u][(p * NG + gr) >> 2][(p * NG + gr) & 3] = 0u;
+                            if (!there || t >= end || !finite[gr]) vm[u].clear(p, gr);
                         }
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) {
@@ -271,15 +305,15 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
                     }
                 }
             }
-            // ---- weights ----
-            Half8 pw[MT];
+            // ---- weights, as the sum of two float16 numbers ----
+            Half8 pw[MT], pl[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 float top = sc[mt][0][0];
 #pragma unroll
                 for (int j = 1; j < 8; ++j) top = fmaxf(top, sc[mt][j >> 2][j & 3]);
-                if (__any(top - ref[mt] > 15.f)) {
-                    const float now = fmaxf(ref[mt], across_rows(top, max_of) - 6.f);
+                if (__any(fmaf(top, to_log2[mt], -ref[mt]) > 15.f)) {
+                    const float now = fmaxf(ref[mt], across_rows(top, max_of) * to_log2[mt] - 6.f);
                     const float keep = exp2f(ref[mt] - now);
                     ref[mt] = now;
                     l[mt] *= keep;
@@ -291,12 +325,16 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
                     float p[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        p[j] = __builtin_amdgcn_exp2f(sc[mt][u][j] - ref[mt]);
+                        p[j] = __builtin_amdgcn_exp2f(fmaf(sc[mt][u][j], to_log2[mt], -ref[mt]));
                         l[mt] += p[j];
                     }
                     // order of the positions as the masks below leave them
-                    pw[mt].h[2 * u] = half2v{(_Float16)p[0], (_Float16)p[2]};
-                    pw[mt].h[2 * u + 1] = half2v{(_Float16)p[1], (_Float16)p[3]};
+#pragma unroll
+                    for (int o = 0; o < 2; ++o) {
+                        const half2v hi = {(_Float16)p[o], (_Float16)p[o + 2]};
+                        pw[mt].h[2 * u + o] = hi;
+                        pl[mt].h[2 * u + o] = half2v{(_Float16)(p[o] - (float)hi[0]), (_Float16)(p[o + 2] - (float)hi[1])};
+                    }
                 }
             }
             // ---- values ----
@@ -307,7 +345,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int o = 0; o < 2; ++o) {
-                        const half2v lo = pair(x.vm[u], o, gr), hi = pair(x.vm[u], o + 2, gr);
+                        const half2v lo = vm[u].at(o, gr), hi = vm[u].at(o + 2, gr);
                         sc2[u][o] = half2v{lo[0], hi[0]};
                         mn2[u][o] = half2v{lo[1], hi[1]};
                     }
@@ -320,36 +358,42 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
                         for (int u = 0; u < 2; ++u)
 #pragma unroll
                             for (int o = 0; o < 2; ++o) {
-                                const uint32_t w = o ? x.v[u][i] >> 8 : x.v[u][i];
-                                const uint32_t biased = h ? (w >> 4 & 0x000F000Fu) | 0x64006400u : (w & 0x000F000Fu) | 0x64006400u;
+                                const uint32_t w = x.v[u][i] >> (8 * o + 4 * h);
+                                const uint32_t biased = (w & 0x000F000Fu) | 0x64006400u;
                                 half2v c;
                                 __builtin_memcpy(&c, &biased, 4);
                                 c -= half2v{(_Float16)1024.f, (_Float16)1024.f};
                                 vf.h[2 * u + o] = __builtin_elementwise_fma(c, sc2[u][o], mn2[u][o]);
                             }
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
+                        for (int mt = 0; mt < MT; ++mt) {
                             acc[mt][2 * i + h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf.v, pw[mt].v, acc[mt][2 * i + h], 0, 0, 0);
+                            acc[mt][2 * i + h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf.v, pl[mt].v, acc[mt][2 * i + h], 0, 0, 0);
+                        }
                     }
             }
         };
 
         const int step = ROWS ? TURN : NW * TURN;
         int t0 = c0 + (ROWS ? 0 : wave * TURN);
+        // two turns' operands in registers: one at work, one on its way; page numbers one turn further ahead
         if (t0 < end) {
-            Turn<D> cur, nxt;
-            int id[2] = {id_of(t0), id_of(t0 + 16)}, id1[2] = {id_of(t0 + step), id_of(t0 + step + 16)};
-            load(cur, t0, id);
+            Turn<D> xa, xb;
+            int ia[2] = {id_of(t0), id_of(t0 + 16)}, ib[2] = {id_of(t0 + step), id_of(t0 + step + 16)};
+            load(xa, t0, ia);
             while (true) {
-                const int t1 = t0 + step;
-                int id2[2] = {id_of(t1 + step), id_of(t1 + step + 16)};
-                if (t1 < end) load(nxt, t1, id1);
-                compute(cur, t0, id);
-                if (t1 >= end) break;
-                cur = nxt;
-                t0 = t1;
-                id[0] = id1[0]; id[1] = id1[1];
-                id1[0] = id2[0]; id1[1] = id2[1];
+                if (t0 + step < end) load(xb, t0 + step, ib);
+                int ic[2] = {id_of(t0 + 2 * step), id_of(t0 + 2 * step + 16)};
+                compute(xa, t0, ia);
+                t0 += step;
+                if (t0 >= end) break;
+                if (t0 + step < end) load(xa, t0 + step, ic);
+                const int id[2] = {id_of(t0 + 2 * step), id_of(t0 + 2 * step + 16)};
+                compute(xb, t0, ib);
+                t0 += step;
+                if (t0 >= end) break;
+                ia[0] = ic[0]; ia[1] = ic[1];
+                ib[0] = id[0]; ib[1] = id[1];
             }
         }
 #pragma unroll
