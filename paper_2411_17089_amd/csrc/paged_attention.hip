@@ -29,7 +29,9 @@ namespace {
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float float2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
+typedef uint32_t word2 __attribute__((ext_vector_type(2)));
 typedef uint32_t word4 __attribute__((ext_vector_type(4)));
 
 constexpr float LOWEST = -0x1p126f;     // where a reference starts: finite, so that no difference of two is NaN
@@ -70,8 +72,13 @@ struct AttentionArgs {
     float scale_log2;
 };
 
+// Lengths and page numbers are read through the constant address space, that is by scalar loads: as vector loads each of them waited
+// for all operands on their way.  Nothing writes them while the kernel runs.
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+__device__ __forceinline__ ScalarInts scalar(const int32_t* p) { return (ScalarInts)(uintptr_t)p; }
+
 // what the chunks of a request are, for the kernels on both sides of the workspace
-__device__ __forceinline__ int span_of(const AttentionArgs& a, int r) { return min(max(a.seq_len[r], 0), a.s.width * a.s.page); }
+__device__ __forceinline__ int span_of(const AttentionArgs& a, int r) { return min(max(scalar(a.seq_len)[r], 0), a.s.width * a.s.page); }
 
 // One turn's operands as they are loaded: the codes, and of the (scale, minimum) pairs of the 32 positions' keys and values, 512
 // bytes, one lane's share.  The pairs go through LDS, where every lane reads those of its four positions: sixteen lanes
@@ -79,7 +86,7 @@ __device__ __forceinline__ int span_of(const AttentionArgs& a, int r) { return m
 template <int D>
 struct Turn {
     static constexpr int NG = D / 64, W = D / 32;
-    uint32_t k[2][W], v[2][W], pairs[NG];
+    uint32_t k[2][W], v[2][W], pairs[2];
 };
 // (scale, minimum) of four positions and NG groups
 template <int D>
@@ -96,40 +103,46 @@ struct Pairs {
 };
 
 template <int D, int MT, bool F32, int NW, bool ROWS>
-__global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const AttentionArgs a) {
+__global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kernel(const AttentionArgs a) {
     constexpr int NG = D / 64, W = D / 32, NT = 2 * W;   // groups, words of codes a lane has per 16 positions, tiles of 16 columns
     const PagedShape& s = a.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m16 = lane & 15, g = lane >> 4;
     const int kv_head = blockIdx.x % s.kv_heads, tile0 = blockIdx.x / s.kv_heads, r = blockIdx.y;
-    const int first = a.row_start[r], m = a.row_start[r + 1] - first, len = a.seq_len[r], span = span_of(a, r);
+    const int first = scalar(a.row_start)[r], m = scalar(a.row_start)[r + 1] - first, len = scalar(a.seq_len)[r], span = span_of(a, r);
     const int chunks = max((span + a.chunk - 1) / a.chunk, 1);
     const int c0 = blockIdx.z * a.chunk, c1 = blockIdx.z == gridDim.z - 1 ? span : min(span, c0 + a.chunk);
     if (c0 > 0 && c0 >= span) return;                                   // chunk 0 is there for empty requests too
     const int64_t all_rows = (int64_t)m * a.group;
-    const int32_t* ids = a.table + (int64_t)r * s.width;
+    const ScalarInts ids = scalar(a.table) + (int64_t)r * s.width;
     const int64_t page_bytes = s.page_bytes();
     const uint8_t* head_base = a.pages + (int64_t)kv_head * s.block_bytes();
     constexpr int TILE_ROWS = MT * 16 * (ROWS ? NW : 1);
     __shared__ uint32_t pair_lds[NW][64 * NG];
+    __shared__ half8 q_lds[ROWS ? NW : 1][F32 ? MT : 1][W][64];         // of float32 q, what float16 leaves
 
     for (int64_t row0 = (int64_t)tile0 * TILE_ROWS; row0 < all_rows; row0 += (int64_t)a.row_tiles * TILE_ROWS) {
         const int64_t wave_row0 = row0 + (ROWS ? wave * MT * 16 : 0);
         if (first + row0 / a.group >= a.rows) return;
         // ---- rows: where they are, how far they see, q ----
-        int token[MT], head[MT], seen[MT];
+        // row, head and whether there is one; worked out again at the end rather than kept
+        auto place = [&](int mt, int& token, int& head) {
+            const int64_t rr = wave_row0 + mt * 16 + m16;
+            const int i = (int)(min(rr, all_rows - 1) / a.group);
+            token = first + i;
+            head = kv_head * a.group + (int)(min(rr, all_rows - 1) - (int64_t)i * a.group);
+            return rr < all_rows && token >= 0 && token < a.rows;
+        };
+        int seen[MT];
         bool real[MT];
-        Half8 q[MT][W], ql[F32 ? MT : 1][W];
+        Half8 q[MT][W];
         float qs[MT][NG], to_log2[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            const int64_t rr = wave_row0 + mt * 16 + m16;
-            const int i = (int)(min(rr, all_rows - 1) / a.group);
-            token[mt] = first + i;
-            head[mt] = kv_head * a.group + (int)(min(rr, all_rows - 1) - (int64_t)i * a.group);
-            real[mt] = rr < all_rows && token[mt] >= 0 && token[mt] < a.rows;
-            seen[mt] = real[mt] ? min(span, len - m + i + 1) : 0;
-            const int64_t at = real[mt] ? token[mt] * a.ldq + (int64_t)head[mt] * D : 0;
+            int token, head;
+            real[mt] = place(mt, token, head);
+            seen[mt] = real[mt] ? min(span, len - m + (token - first) + 1) : 0;
+            const int64_t at = real[mt] ? token * a.ldq + (int64_t)head * D : 0;
             float x[W][8], big = 0.f;
 #pragma unroll
             for (int st = 0; st < W; ++st) {
@@ -164,13 +177,16 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
 #pragma unroll
             for (int st = 0; st < W; ++st) {
                 constexpr int order[8] = {0, 4, 1, 5, 2, 6, 3, 7};      // columns as the masks below leave them
+                Half8 rest;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float y = x[st][order[e]] * up * ((e & 2) ? 0.0625f : 1.f);
                     const _Float16 hi = (_Float16)y;
                     q[mt][st].v[e] = hi;
-                    if constexpr (F32) ql[mt][st].v[e] = (_Float16)(y - (float)hi);
+                    if constexpr (F32) rest.v[e] = (_Float16)(y - (float)hi);
                 }
+                // the waves that share rows write the same
+                if constexpr (F32) q_lds[ROWS ? wave : 0][mt][st][lane] = rest.v;
             }
         }
         // positions that every / any row of the wave sees
@@ -190,51 +206,48 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
 
         float ref[MT], l[MT];
         float4v acc[MT][NT];
-        float spoilt[MT][NG];                                           // NaN once a row has seen values that are not finite in a masked turn
+        float spoilt[MT];                                               // NaN once a row has seen values that are not finite in a masked turn
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             ref[mt] = LOWEST;
             l[mt] = 0.f;
 #pragma unroll
             for (int t = 0; t < NT; ++t) acc[mt][t] = float4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int gr = 0; gr < NG; ++gr) spoilt[mt][gr] = 0.f;
+            spoilt[mt] = 0.f;
         }
 
-        const uint32_t k_lane = m16 * (D / 2) + g * (D / 8), v_lane = s.page * (D / 2) + g * (2 * D) + m16 * (D / 8),
-                       p_lane = s.page * D + (lane & 16 ? s.page * (NG * 4) : 0) + m16 * (NG * 4);
-        auto id_of = [&](int t) { return t < end ? ids[t >> s.page_log2] : -1; };
+        const int k_lane = m16 * (D / 2) + g * (D / 8), v_lane = s.page * (D / 2) + g * (2 * D) + m16 * (D / 8),
+                  p_lane = s.page * D + (NG == 2 ? (lane & 32 ? s.page * 8 : 0) + (lane & 31) * 4 : (lane & 16 ? s.page * 4 : 0) + m16 * 4);
+        auto id_of = [&](int t) { return ids[min(t, end - 1) >> s.page_log2]; };     // those behind the end are not used
         auto load = [&](Turn<D>& x, int t0, const int (&id)[2]) {
-            const uint8_t* pb[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                // a turn's halves that lie behind the end or outside the pool read the pool's first page and are masked
+                // a half of a turn that lies outside the pool reads its first page and is masked; one behind the end reads what is there
                 const int tp = (t0 + 16 * u) & (s.page - 1);
                 const uint8_t* b = head_base + (int64_t)((unsigned)id[u] < (unsigned)s.n_pages ? id[u] : 0) * page_bytes;
-                pb[u] = b + tp * (NG * 4);
-                const uint8_t* cb = b + tp * (D / 2);
+                const __amdgpu_buffer_rsrc_t block = __builtin_amdgcn_make_buffer_rsrc((void*)b, 0, (int)s.block_bytes(), 0x00027000);
                 if constexpr (D == 128) {
-                    const word4 kw = *reinterpret_cast<const word4*>(cb + k_lane), vw = *reinterpret_cast<const word4*>(cb + v_lane);
+                    const word4 kw = __builtin_amdgcn_raw_buffer_load_b128(block, k_lane, tp * (D / 2), 0),
+                                vw = __builtin_amdgcn_raw_buffer_load_b128(block, v_lane, tp * (D / 2), 0);
 #pragma unroll
                     for (int i = 0; i < W; ++i) { x.k[u][i] = kw[i]; x.v[u][i] = vw[i]; }
                 } else {
-                    const uint2 kw = *reinterpret_cast<const uint2*>(cb + k_lane), vw = *reinterpret_cast<const uint2*>(cb + v_lane);
-                    x.k[u][0] = kw.x; x.k[u][1] = kw.y; x.v[u][0] = vw.x; x.v[u][1] = vw.y;
+                    const word2 kw = __builtin_amdgcn_raw_buffer_load_b64(block, k_lane, tp * (D / 2), 0),
+                                vw = __builtin_amdgcn_raw_buffer_load_b64(block, v_lane, tp * (D / 2), 0);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) { x.k[u][i] = kw[i]; x.v[u][i] = vw[i]; }
                 }
-            }
-            const uint32_t* pp = reinterpret_cast<const uint32_t*>((lane & 32 ? pb[1] : pb[0]) + p_lane);
-            if constexpr (D == 128) {
-                const uint2 w = *reinterpret_cast<const uint2*>(pp);
-                x.pairs[0] = w.x; x.pairs[1] = w.y;
-            } else {
-                x.pairs[0] = *pp;
+                x.pairs[u] = __builtin_amdgcn_raw_buffer_load_b32(block, p_lane, tp * (NG * 4), 0);
             }
         };
+        // in a register, so that masking and setting the upper bits are one instruction (with two literals they are two)
+        uint32_t magic = 0x64006400u;
+        asm("" : "+v"(magic));
         auto compute = [&](const Turn<D>& x, int t0, const int (&id)[2]) {
-            const bool masked = t0 + TURN > all_see || t0 + TURN > c1 || (unsigned)id[0] >= (unsigned)s.n_pages || (unsigned)id[1] >= (unsigned)s.n_pages;
+            const bool masked = t0 + TURN > min(all_see, c1) || (unsigned)id[0] >= (unsigned)s.n_pages || (unsigned)id[1] >= (unsigned)s.n_pages;
             uint32_t* mine = pair_lds[wave];
-            if constexpr (D == 128) *reinterpret_cast<uint2*>(mine + 2 * lane) = make_uint2(x.pairs[0], x.pairs[1]);
-            else mine[lane] = x.pairs[0];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) mine[u * 32 * NG + (NG == 2 ? lane : lane & 31)] = x.pairs[u];
             wave_fence();
             auto pairs_of = [&](int u, int values) {
                 Pairs<D> r;
@@ -245,24 +258,39 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
             };
             // ---- scores, in units of 2^to_log2 ----
             float sc[MT][2][4];
+            float4v c[2][MT][NG];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float4v c[MT][NG];
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                    for (int gr = 0; gr < NG; ++gr) c[mt][gr] = float4v{0.f, 0.f, 0.f, 0.f};
+                    for (int gr = 0; gr < NG; ++gr) c[u][mt][gr] = float4v{0.f, 0.f, 0.f, 0.f};
+            auto score = [&](int u, int st, const half8 (&ql)[MT]) {
+                Half8 kf;
+                const uint32_t w = x.k[u][st], w8 = w >> 8;
+                kf.w[0] = w & 0x000F000Fu; kf.w[1] = w & 0x00F000F0u; kf.w[2] = w8 & 0x000F000Fu; kf.w[3] = w8 & 0x00F000F0u;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    c[u][mt][st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf.v, q[mt][st].v, c[u][mt][st / 2], 0, 0, 0);
+                    if constexpr (F32) c[u][mt][st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf.v, ql[mt], c[u][mt][st / 2], 0, 0, 0);
+                }
+            };
+            half8 ql[MT];
+            if constexpr (F32) {
+                // both halves of the turn with one read of a step's rest
 #pragma unroll
                 for (int st = 0; st < W; ++st) {
-                    Half8 kf;
-                    const uint32_t w = x.k[u][st], w8 = w >> 8;
-                    kf.w[0] = w & 0x000F000Fu; kf.w[1] = w & 0x00F000F0u; kf.w[2] = w8 & 0x000F000Fu; kf.w[3] = w8 & 0x00F000F0u;
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        c[mt][st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf.v, q[mt][st].v, c[mt][st / 2], 0, 0, 0);
-                        if constexpr (F32) c[mt][st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf.v, ql[mt][st].v, c[mt][st / 2], 0, 0, 0);
-                    }
+                    for (int mt = 0; mt < MT; ++mt) ql[mt] = q_lds[ROWS ? wave : 0][mt][st][lane];
+                    score(0, st, ql);
+                    score(1, st, ql);
                 }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if constexpr (!F32)
+#pragma unroll
+                    for (int st = 0; st < W; ++st) score(u, st, ql);
                 const Pairs<D> km = pairs_of(u, 0);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
@@ -272,7 +300,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
 #pragma unroll
                         for (int gr = 0; gr < NG; ++gr) {
                             const half2v sm = km.at(p, gr);
-                            t = fmaf((float)sm[0], c[mt][gr][p], fmaf((float)sm[1], qs[mt][gr], t));
+                            t = fmaf((float)sm[0], c[u][mt][gr][p], fmaf((float)sm[1], qs[mt][gr], t));
                         }
                         sc[mt][u][p] = t;
                     }
@@ -282,25 +310,26 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
             if (masked) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const bool there = (unsigned)id[u] < (unsigned)s.n_pages;
+                    const int all = (unsigned)id[u] < (unsigned)s.n_pages ? end : 0;
 #pragma unroll
                     for (int p = 0; p < 4; ++p) {
                         const int t = t0 + 16 * u + 4 * g + p;
-                        bool finite[NG];
+                        float poison = 0.f;                             // NaN for values that are not finite
 #pragma unroll
                         for (int gr = 0; gr < NG; ++gr) {
                             const half2v sm = vm[u].at(p, gr);
-                            finite[gr] = fabsf((float)sm[0]) < INFINITY && fabsf((float)sm[1]) < INFINITY;
-                            // positions that a row does not see must not reach its sum, not even as 0 times NaN
-                            if (!there || t >= end || !finite[gr]) vm[u].clear(p, gr);
+                            poison += (float)sm[0] * 0.f + (float)sm[1] * 0.f;
                         }
+                        // positions that a row does not see must not reach its sum, not even as 0 times NaN
+                        const bool out = t >= all || poison != 0.f;
+#pragma unroll
+                        for (int gr = 0; gr < NG; ++gr)
+                            if (out) vm[u].clear(p, gr);
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) {
-                            const bool sees = there && t < c1 && t < seen[mt];
+                            const bool sees = t < min(all, seen[mt]);
                             if (!sees) sc[mt][u][p] = -INFINITY;
-#pragma unroll
-                            for (int gr = 0; gr < NG; ++gr)
-                                if (sees && !finite[gr]) spoilt[mt][gr] = NAN;
+                            spoilt[mt] += sees ? poison : 0.f;
                         }
                     }
                 }
@@ -331,9 +360,9 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
                     // order of the positions as the masks below leave them
 #pragma unroll
                     for (int o = 0; o < 2; ++o) {
-                        const half2v hi = {(_Float16)p[o], (_Float16)p[o + 2]};
+                        const half2v hi = __builtin_convertvector((float2v{p[o], p[o + 2]}), half2v);
                         pw[mt].h[2 * u + o] = hi;
-                        pl[mt].h[2 * u + o] = half2v{(_Float16)(p[o] - (float)hi[0]), (_Float16)(p[o + 2] - (float)hi[1])};
+                        pl[mt].h[2 * u + o] = __builtin_convertvector((float2v{fmaf((float)hi[0], -1.f, p[o]), fmaf((float)hi[1], -1.f, p[o + 2])}), half2v);
                     }
                 }
             }
@@ -358,11 +387,12 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
                         for (int u = 0; u < 2; ++u)
 #pragma unroll
                             for (int o = 0; o < 2; ++o) {
-                                const uint32_t w = x.v[u][i] >> (8 * o + 4 * h);
-                                const uint32_t biased = (w & 0x000F000Fu) | 0x64006400u;
+                                // 1024 + code, or 1024 + 16 code where the code stays in the upper bits: both come out exactly
+                                const uint32_t biased = (x.v[u][i] >> (8 * o) & (h ? 0x00F000F0u : 0x000F000Fu)) | magic;
                                 half2v c;
                                 __builtin_memcpy(&c, &biased, 4);
-                                c -= half2v{(_Float16)1024.f, (_Float16)1024.f};
+                                c = h ? __builtin_elementwise_fma(c, half2v{(_Float16)0.0625f, (_Float16)0.0625f}, half2v{(_Float16)-64.f, (_Float16)-64.f})
+                                      : c - half2v{(_Float16)1024.f, (_Float16)1024.f};
                                 vf.h[2 * u + o] = __builtin_elementwise_fma(c, sc2[u][o], mn2[u][o]);
                             }
 #pragma unroll
@@ -381,13 +411,15 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
             Turn<D> xa, xb;
             int ia[2] = {id_of(t0), id_of(t0 + 16)}, ib[2] = {id_of(t0 + step), id_of(t0 + step + 16)};
             load(xa, t0, ia);
+            // loads behind the end (of pages that are there: id_of stays below it) keep the number of loads on their way the same on every path,
+            // so that a turn waits for its own only
             while (true) {
-                if (t0 + step < end) load(xb, t0 + step, ib);
-                int ic[2] = {id_of(t0 + 2 * step), id_of(t0 + 2 * step + 16)};
+                load(xb, t0 + step, ib);
+                const int ic[2] = {id_of(t0 + 2 * step), id_of(t0 + 2 * step + 16)};
                 compute(xa, t0, ia);
                 t0 += step;
                 if (t0 >= end) break;
-                if (t0 + step < end) load(xa, t0 + step, ic);
+                load(xa, t0 + step, ic);
                 const int id[2] = {id_of(t0 + 2 * step), id_of(t0 + 2 * step + 16)};
                 compute(xb, t0, ib);
                 t0 += step;
@@ -399,27 +431,23 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const Attentio
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             l[mt] = across_rows(l[mt], sum_of);
+            const float bad = across_rows(spoilt[mt], sum_of);
 #pragma unroll
-            for (int gr = 0; gr < NG; ++gr) {
-                const float bad = across_rows(spoilt[mt][gr], sum_of);
-#pragma unroll
-                for (int t = 4 * gr; t < 4 * gr + 4; ++t)
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) acc[mt][t][p] += bad;
-            }
+            for (int t = 0; t < NT; ++t) acc[mt][t] += bad;
         }
         // writes columns 64 gr + 16 g + 4 p .. + 3 of one row from what = acc over (w, h)
         auto put = [&](int mt, int p, int gr, const float (&what)[4], float ref_, float l_) {
-            if (!real[mt]) return;
+            int token, head;
+            if (!place(mt, token, head)) return;
             const int col = 64 * gr + (4 * g + p) * 4;
             if (chunks == 1 || gridDim.z == 1) {
                 const float inv = l_ == 0.f ? 0.f : 1.f / l_;
                 half4 out;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) out[e] = (_Float16)(l_ == 0.f ? 0.f : what[e] * inv);
-                *reinterpret_cast<half4*>(a.z + token[mt] * a.ldz + (int64_t)head[mt] * D + col) = out;
+                *reinterpret_cast<half4*>(a.z + token * a.ldz + (int64_t)head * D + col) = out;
             } else {
-                const int64_t slot = ((int64_t)blockIdx.z * a.rows + token[mt]) * s.heads + head[mt];
+                const int64_t slot = ((int64_t)blockIdx.z * a.rows + token) * s.heads + head;
                 *reinterpret_cast<float4v*>(a.acc + slot * D + col) = float4v{what[0], what[1], what[2], what[3]};
                 if (col == 0) *reinterpret_cast<float2*>(a.ml + slot * 2) = make_float2(ref_, l_);
             }
