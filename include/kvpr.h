@@ -473,7 +473,7 @@ typedef struct {
     int32_t head_dim;      /* 64 or 128                                                         */
     int32_t page_size;     /* positions per page: 16, 32, 64, 128 or 256                        */
     int32_t n_pages;       /* pages in the pool; n_pages * page_size < 2^31                     */
-    int32_t table_width;   /* entries per request in block_table; table_width * page_size < 2^31 */
+    int32_t table_width;   /* entries per request in block_table; table_width * page_size <= 2^30 */
 } kvpr_paged_desc;
 
 size_t kvpr_page_bytes(const kvpr_paged_desc* desc);   /* 0 for a description that the calls refuse */

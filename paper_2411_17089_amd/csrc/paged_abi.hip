@@ -19,7 +19,7 @@ int check_shape(const kvpr_paged_desc* d, kvpr::PagedShape& s) {
     if (d->page_size < 16 || d->page_size > 256 || (d->page_size & (d->page_size - 1)))
         return fail(KVPR_E_INVAL, "page_size=%d must be 16, 32, 64, 128 or 256", d->page_size);
     if (d->n_pages < 1 || (int64_t)d->n_pages * d->page_size > 0x7fffffff) return fail(KVPR_E_RANGE, "n_pages=%d out of range (slots are 32-bit)", d->n_pages);
-    if (d->table_width < 1 || (int64_t)d->table_width * d->page_size > 0x7fffffff) return fail(KVPR_E_RANGE, "table_width=%d out of range", d->table_width);
+    if (d->table_width < 1 || (int64_t)d->table_width * d->page_size > (1 << 30)) return fail(KVPR_E_RANGE, "table_width=%d out of range", d->table_width);
     s = kvpr::PagedShape{d->n_heads, d->n_kv_heads, d->head_dim, d->page_size, log2_of(d->page_size), d->n_pages, d->table_width};
     return KVPR_OK;
 }
@@ -95,6 +95,7 @@ extern "C" int kvpr_paged_attention(const kvpr_paged_desc* desc, const void* q, 
     if (int rc = check_shape(desc, s)) return rc;
     if (int rc = check_batch(n_requests, n_rows, max_new, max_len)) return rc;
     if (q_type != KVPR_F16 && q_type != KVPR_F32) return fail(KVPR_E_INVAL, "q_type must be KVPR_F16 or KVPR_F32");
+    if ((int64_t)n_rows * (s.heads / s.kv_heads) > (1 << 30)) return fail(KVPR_E_RANGE, "n_rows=%d times %d heads per key/value head is beyond 2^30", n_rows, s.heads / s.kv_heads);
     const int64_t cols = (int64_t)s.heads * s.d;
     if (ldq < cols || ldq % 8 || ldz < cols || ldz % 8) return fail(KVPR_E_INVAL, "need ldq, ldz >= %lld and multiples of 8", (long long)cols);
     if (n_rows == 0) return KVPR_OK;

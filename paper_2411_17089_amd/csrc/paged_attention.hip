@@ -113,25 +113,63 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
     const int chunks = max((span + a.chunk - 1) / a.chunk, 1);
     const int c0 = blockIdx.z * a.chunk, c1 = blockIdx.z == gridDim.z - 1 ? span : min(span, c0 + a.chunk);
     if (c0 > 0 && c0 >= span) return;                                   // chunk 0 is there for empty requests too
-    const int64_t all_rows = (int64_t)m * a.group;
+    const int all_rows = (first < 0 ? 0 : max(min(m, a.rows - first), 0)) * a.group;     // at most 2^30
     const ScalarInts ids = scalar(a.table) + (int64_t)r * s.width;
     const int64_t page_bytes = s.page_bytes();
     const uint8_t* head_base = a.pages + (int64_t)kv_head * s.block_bytes();
     constexpr int TILE_ROWS = MT * 16 * (ROWS ? NW : 1);
     __shared__ uint32_t pair_lds[NW][64 * NG];
+    __shared__ float part[ROWS ? 1 : NW][4][NT][64];
+    __shared__ float2 ml[NW][16];
     __shared__ half8 q_lds[ROWS ? NW : 1][F32 ? MT : 1][W][64];         // of float32 q, what float16 leaves
 
-    for (int64_t row0 = (int64_t)tile0 * TILE_ROWS; row0 < all_rows; row0 += (int64_t)a.row_tiles * TILE_ROWS) {
-        const int64_t wave_row0 = row0 + (ROWS ? wave * MT * 16 : 0);
-        if (first + row0 / a.group >= a.rows) return;
+    for (int row0 = tile0 * TILE_ROWS; row0 < all_rows; row0 += a.row_tiles * TILE_ROWS) {
+        const int wave_row0 = row0 + (ROWS ? wave * MT * 16 : 0), live = min(all_rows - wave_row0, MT * 16);
+        // positions that every / any row of the wave sees: those of its first and its last row
+        const int see0 = len - m + 1, all_see = min(span, see0 + wave_row0 / a.group),
+                  any_see = live > 0 ? min(span, see0 + (wave_row0 + live - 1) / a.group) : 0;
+        const int end = min(c1, any_see);
+        const int k_lane = m16 * (D / 2) + g * (D / 8), v_lane = s.page * (D / 2) + g * (2 * D) + m16 * (D / 8),
+                  p_lane = s.page * D + (NG == 2 ? (lane & 32 ? s.page * 8 : 0) + (lane & 31) * 4 : (lane & 16 ? s.page * 4 : 0) + m16 * 4);
+        auto id_of = [&](int t) { return ids[min(t, end - 1) >> s.page_log2]; };     // those behind the end are not used
+        auto load = [&](Turn<D>& x, int t0, const int (&id)[2]) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                // a half of a turn that lies outside the pool reads its first page and is masked; one behind the end reads what is there
+                const int tp = (t0 + 16 * u) & (s.page - 1);
+                const uint8_t* b = head_base + (int64_t)((unsigned)id[u] < (unsigned)s.n_pages ? id[u] : 0) * page_bytes;
+                const __amdgpu_buffer_rsrc_t block = __builtin_amdgcn_make_buffer_rsrc((void*)b, 0, (int)s.block_bytes(), 0x00027000);
+                if constexpr (D == 128) {
+                    const word4 kw = __builtin_amdgcn_raw_buffer_load_b128(block, k_lane, tp * (D / 2), 0),
+                                vw = __builtin_amdgcn_raw_buffer_load_b128(block, v_lane, tp * (D / 2), 0);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) { x.k[u][i] = kw[i]; x.v[u][i] = vw[i]; }
+                } else {
+                    const word2 kw = __builtin_amdgcn_raw_buffer_load_b64(block, k_lane, tp * (D / 2), 0),
+                                vw = __builtin_amdgcn_raw_buffer_load_b64(block, v_lane, tp * (D / 2), 0);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) { x.k[u][i] = kw[i]; x.v[u][i] = vw[i]; }
+                }
+                x.pairs[u] = __builtin_amdgcn_raw_buffer_load_b32(block, p_lane, tp * (NG * 4), 0);
+            }
+        };
+        const int step = ROWS ? TURN : NW * TURN;
+        int t0 = c0 + (ROWS ? 0 : wave * TURN);
+        // two turns' operands in registers: one at work, one on its way; page numbers one turn further ahead
+        Turn<D> xa, xb;
+        int ia[2], ib[2];
+        const bool any_turn = t0 < end;
+        if (any_turn) {
+            ia[0] = id_of(t0); ia[1] = id_of(t0 + 16); ib[0] = id_of(t0 + step); ib[1] = id_of(t0 + step + 16);
+            load(xa, t0, ia);
+        }
         // ---- rows: where they are, how far they see, q ----
         // row, head and whether there is one; worked out again at the end rather than kept
         auto place = [&](int mt, int& token, int& head) {
-            const int64_t rr = wave_row0 + mt * 16 + m16;
-            const int i = (int)(min(rr, all_rows - 1) / a.group);
+            const int rr = wave_row0 + mt * 16 + m16, there = min(rr, all_rows - 1), i = there / a.group;
             token = first + i;
-            head = kv_head * a.group + (int)(min(rr, all_rows - 1) - (int64_t)i * a.group);
-            return rr < all_rows && token >= 0 && token < a.rows;
+            head = kv_head * a.group + there - i * a.group;
+            return rr < all_rows;
         };
         int seen[MT];
         bool real[MT];
@@ -189,57 +227,17 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
                 if constexpr (F32) q_lds[ROWS ? wave : 0][mt][st][lane] = rest.v;
             }
         }
-        // positions that every / any row of the wave sees
-        int all_see = 0x7fffffff, any_see = 0;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            all_see = min(all_see, real[mt] ? seen[mt] : 0x7fffffff);
-            any_see = max(any_see, seen[mt]);
-        }
-        for (int o = 1; o < 16; o <<= 1) {
-            all_see = min(all_see, __shfl_xor(all_see, o));
-            any_see = max(any_see, __shfl_xor(any_see, o));
-        }
-        all_see = __builtin_amdgcn_readfirstlane(all_see);
-        any_see = __builtin_amdgcn_readfirstlane(any_see);
-        const int end = min(c1, any_see);
 
         float ref[MT], l[MT];
         float4v acc[MT][NT];
-        float spoilt[MT];                                               // NaN once a row has seen values that are not finite in a masked turn
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             ref[mt] = LOWEST;
             l[mt] = 0.f;
 #pragma unroll
             for (int t = 0; t < NT; ++t) acc[mt][t] = float4v{0.f, 0.f, 0.f, 0.f};
-            spoilt[mt] = 0.f;
         }
 
-        const int k_lane = m16 * (D / 2) + g * (D / 8), v_lane = s.page * (D / 2) + g * (2 * D) + m16 * (D / 8),
-                  p_lane = s.page * D + (NG == 2 ? (lane & 32 ? s.page * 8 : 0) + (lane & 31) * 4 : (lane & 16 ? s.page * 4 : 0) + m16 * 4);
-        auto id_of = [&](int t) { return ids[min(t, end - 1) >> s.page_log2]; };     // those behind the end are not used
-        auto load = [&](Turn<D>& x, int t0, const int (&id)[2]) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                // a half of a turn that lies outside the pool reads its first page and is masked; one behind the end reads what is there
-                const int tp = (t0 + 16 * u) & (s.page - 1);
-                const uint8_t* b = head_base + (int64_t)((unsigned)id[u] < (unsigned)s.n_pages ? id[u] : 0) * page_bytes;
-                const __amdgpu_buffer_rsrc_t block = __builtin_amdgcn_make_buffer_rsrc((void*)b, 0, (int)s.block_bytes(), 0x00027000);
-                if constexpr (D == 128) {
-                    const word4 kw = __builtin_amdgcn_raw_buffer_load_b128(block, k_lane, tp * (D / 2), 0),
-                                vw = __builtin_amdgcn_raw_buffer_load_b128(block, v_lane, tp * (D / 2), 0);
-#pragma unroll
-                    for (int i = 0; i < W; ++i) { x.k[u][i] = kw[i]; x.v[u][i] = vw[i]; }
-                } else {
-                    const word2 kw = __builtin_amdgcn_raw_buffer_load_b64(block, k_lane, tp * (D / 2), 0),
-                                vw = __builtin_amdgcn_raw_buffer_load_b64(block, v_lane, tp * (D / 2), 0);
-#pragma unroll
-                    for (int i = 0; i < W; ++i) { x.k[u][i] = kw[i]; x.v[u][i] = vw[i]; }
-                }
-                x.pairs[u] = __builtin_amdgcn_raw_buffer_load_b32(block, p_lane, tp * (NG * 4), 0);
-            }
-        };
         // in a register, so that masking and setting the upper bits are one instruction (with two literals they are two)
         uint32_t magic = 0x64006400u;
         asm("" : "+v"(magic));
@@ -329,7 +327,7 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
                         for (int mt = 0; mt < MT; ++mt) {
                             const bool sees = t < min(all, seen[mt]);
                             if (!sees) sc[mt][u][p] = -INFINITY;
-                            spoilt[mt] += sees ? poison : 0.f;
+                            l[mt] += sees ? poison : 0.f;              // the row is NaN
                         }
                     }
                 }
@@ -404,13 +402,7 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
             }
         };
 
-        const int step = ROWS ? TURN : NW * TURN;
-        int t0 = c0 + (ROWS ? 0 : wave * TURN);
-        // two turns' operands in registers: one at work, one on its way; page numbers one turn further ahead
-        if (t0 < end) {
-            Turn<D> xa, xb;
-            int ia[2] = {id_of(t0), id_of(t0 + 16)}, ib[2] = {id_of(t0 + step), id_of(t0 + step + 16)};
-            load(xa, t0, ia);
+        if (any_turn) {
             // loads behind the end (of pages that are there: id_of stays below it) keep the number of loads on their way the same on every path,
             // so that a turn waits for its own only
             while (true) {
@@ -431,68 +423,65 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             l[mt] = across_rows(l[mt], sum_of);
-            const float bad = across_rows(spoilt[mt], sum_of);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) acc[mt][t] += bad;
         }
-        // writes columns 64 gr + 16 g + 4 p .. + 3 of one row from what = acc over (w, h)
-        auto put = [&](int mt, int p, int gr, const float (&what)[4], float ref_, float l_) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            if (row0 + mt * 16 >= all_rows) break;
             int token, head;
-            if (!place(mt, token, head)) return;
-            const int col = 64 * gr + (4 * g + p) * 4;
-            if (chunks == 1 || gridDim.z == 1) {
-                const float inv = l_ == 0.f ? 0.f : 1.f / l_;
-                half4 out;
+            const bool there = place(mt, token, head);
+            float top = ref[mt], sum = l[mt];
+            // columns 64 gr + 16 g + 4 p .. + 3 of one row from acc over (w, h)
+            auto put = [&](int p, int gr, const float (&what)[4]) {
+                if (!there) return;
+                const int col = 64 * gr + (4 * g + p) * 4;
+                if (chunks == 1 || gridDim.z == 1) {
+                    const float inv = 1.f / sum;
+                    half4 out;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) out[e] = (_Float16)(l_ == 0.f ? 0.f : what[e] * inv);
-                *reinterpret_cast<half4*>(a.z + token * a.ldz + (int64_t)head * D + col) = out;
-            } else {
-                const int64_t slot = ((int64_t)blockIdx.z * a.rows + token) * s.heads + head;
-                *reinterpret_cast<float4v*>(a.acc + slot * D + col) = float4v{what[0], what[1], what[2], what[3]};
-                if (col == 0) *reinterpret_cast<float2*>(a.ml + slot * 2) = make_float2(ref_, l_);
-            }
-        };
-        if constexpr (ROWS) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+                    for (int e = 0; e < 4; ++e) out[e] = (_Float16)(sum == 0.f ? 0.f : what[e] * inv);
+                    *reinterpret_cast<half4*>(a.z + token * a.ldz + (int64_t)head * D + col) = out;
+                } else {
+                    const int64_t slot = ((int64_t)blockIdx.z * a.rows + token) * s.heads + head;
+                    *reinterpret_cast<float4v*>(a.acc + slot * D + col) = float4v{what[0], what[1], what[2], what[3]};
+                    if (col == 0) *reinterpret_cast<float2*>(a.ml + slot * 2) = make_float2(top, sum);
+                }
+            };
+            if constexpr (ROWS) {
 #pragma unroll
                 for (int p = 0; p < 4; ++p)
 #pragma unroll
                     for (int gr = 0; gr < NG; ++gr) {
                         const float what[4] = {acc[mt][4 * gr][p], acc[mt][4 * gr + 1][p], acc[mt][4 * gr + 2][p], acc[mt][4 * gr + 3][p]};
-                        put(mt, p, gr, what, ref[mt], l[mt]);
+                        put(p, gr, what);
                     }
-        } else {
-            // the waves' sums meet in LDS, a tile of rows at a time; wave w then has the columns of p = w (and w + 4 ..)
-            __shared__ float part[NW][4][NT][64];
-            __shared__ float2 ml[NW][16];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
+            } else {
+                // the waves' sums meet in LDS, a tile of rows at a time; wave w then has the columns of p = w
+                if (mt || row0 != tile0 * TILE_ROWS) __syncthreads();
+                if (g == 0) ml[wave][m16] = make_float2(top, sum);
                 __syncthreads();
-                if (g == 0) ml[wave][m16] = make_float2(ref[mt], l[mt]);
-                __syncthreads();
-                float top = LOWEST, sum = 0.f;
+                float all_top = LOWEST;
+                sum = 0.f;
 #pragma unroll
-                for (int w = 0; w < NW; ++w) top = fmaxf(top, ml[w][m16].x);
+                for (int w = 0; w < NW; ++w) all_top = fmaxf(all_top, ml[w][m16].x);
 #pragma unroll
-                for (int w = 0; w < NW; ++w) sum += ml[w][m16].y * exp2f(ml[w][m16].x - top);
-                const float mine = exp2f(ref[mt] - top);
+                for (int w = 0; w < NW; ++w) sum += ml[w][m16].y * exp2f(ml[w][m16].x - all_top);
+                const float mine = exp2f(top - all_top);
+                top = all_top;
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int p = 0; p < 4; ++p) part[wave][p][t][lane] = acc[mt][t][p] * mine;
                 __syncthreads();
-                for (int j = wave; j < 4 * NG; j += NW) {
-                    const int p = j & 3, gr = j >> 2;
+#pragma unroll
+                for (int gr = 0; gr < NG; ++gr) {
                     float what[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int w = 0; w < NW; ++w)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) what[e] += part[w][p][4 * gr + e][lane];
-                    put(mt, p, gr, what, top, sum);
+                        for (int e = 0; e < 4; ++e) what[e] += part[w][wave][4 * gr + e][lane];
+                    put(wave, gr, what);
                 }
             }
-            __syncthreads();
         }
     }
 }
@@ -543,7 +532,7 @@ Cut cut_of(const PagedShape& s, int n, int max_new, int max_len, bool) {
     c.row_tiles = (int)std::min<int64_t>((r + tile - 1) / tile, 65535 / 8);
     const int64_t len = std::min<int64_t>(max_len, (int64_t)s.width * s.page);
     const int64_t units = (int64_t)n * s.kv_heads * c.row_tiles;
-    const int64_t want = std::max<int64_t>(1, 1024 / units), least = c.rows ? 512 : NW * TURN;
+    const int64_t want = std::max<int64_t>(1, (c.rows ? 512 : 1024) / units), least = c.rows ? 512 : NW * TURN;
     int64_t chunk = std::max(least, (len + want - 1) / want);
     if (!c.rows) chunk = std::min<int64_t>(chunk, 2048);
     chunk = (chunk + NW * TURN - 1) / (NW * TURN) * (NW * TURN);
