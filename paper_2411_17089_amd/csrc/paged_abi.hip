@@ -110,6 +110,7 @@ extern "C" int kvpr_paged_attention(const kvpr_paged_desc* desc, const void* q, 
 static int check_verify(int n_requests, int n_rows, int vocab) {
     if (n_requests < 1 || n_requests > kvpr::kMaxRequests || n_rows < 0 || vocab < 1 || vocab > (1 << 24))
         return fail(KVPR_E_RANGE, "n_requests=%d (1 to %d) n_rows=%d vocab=%d (1 to 2^24) out of range", n_requests, kvpr::kMaxRequests, n_rows, vocab);
+    if ((int64_t)n_rows * ((vocab + 2047) / 2048) > 0x7fffff) return fail(KVPR_E_RANGE, "n_rows=%d of vocab=%d logits are too many", n_rows, vocab);
     return KVPR_OK;
 }
 
