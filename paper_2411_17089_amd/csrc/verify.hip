@@ -22,31 +22,37 @@ constexpr int THREADS = 256, WAVES = THREADS / 64;
 // a logit that takes part; NaN counts as -inf
 __device__ __forceinline__ float logit(float v) { return v == v ? v : -INFINITY; }
 
-// exp(x) for x <= 0, to 2^-46: x = k ln 2 + r, the Taylor polynomial of degree 11 in |r| <= 0.347 (the rest of the series is below
-// 0.347^12 / 12! = 7e-15), ldexp.  A third of the instructions of the library function.
-__device__ __forceinline__ double exp_of(double x) {
-    x = fmax(x, -800.0);                                   // 0 from -745 on
-    const double k = rint(x * 1.4426950408889634);
-    const double r = fma(k, -1.9082149292705877e-10, fma(k, -0.6931471803691238, x));
-    double p = 1.0 / 39916800.0;
-    p = fma(p, r, 1.0 / 3628800.0);
-    p = fma(p, r, 1.0 / 362880.0);
-    p = fma(p, r, 1.0 / 40320.0);
-    p = fma(p, r, 1.0 / 5040.0);
-    p = fma(p, r, 1.0 / 720.0);
-    p = fma(p, r, 1.0 / 120.0);
-    p = fma(p, r, 1.0 / 24.0);
-    p = fma(p, r, 1.0 / 6.0);
-    p = fma(p, r, 0.5);
-    p = fma(p, r, 1.0);
-    p = fma(p, r, 1.0);
-    return __builtin_ldexp(p, (int)k);
+// 2^t for t <= 0: t = k + f with |f| <= 1/2 (adding 1.5 2^52 leaves k in the low word), the polynomial of degree 9 that meets 2^f in the 10
+// Chebyshev points of that interval (off by 2 10^-14 at most), ldexp.  16 instructions of 64 bits where the library's exp and the steps
+// around it take 40: those bound the reading of the logits.
+__device__ __forceinline__ double exp2_of(double t) {
+    const double big = 6755399441055744.0, kd = t + big, f = t - (kd - big);
+    double p = 1.0212097549811005e-07;
+    p = fma(p, f, 1.3259945262689143e-06);
+    p = fma(p, f, 1.5252640059770786e-05);
+    p = fma(p, f, 0.00015403432339553542);
+    p = fma(p, f, 0.001333355825801874);
+    p = fma(p, f, 0.009618129195951041);
+    p = fma(p, f, 0.05550410866428854);
+    p = fma(p, f, 0.24022650695631514);
+    p = fma(p, f, 0.6931471805599526);
+    p = fma(p, f, 1.000000000000014);
+    return __builtin_ldexp(p, __double2loint(kd));
 }
 
-// exp((v - top) / T), 1 at the top itself (also an infinite one)
-__device__ __forceinline__ double weight(float v, float top, double inv_t) {
-    return exp_of(v == top ? 0.0 : ((double)v - (double)top) * inv_t);
-}
+// exp((v - top) / T) of one row; with an infinite top 1 where the logit is infinite too and 0 elsewhere
+struct Weight {
+    float top, low;                 // low: logits that far down have weight 0 whatever they are
+    double c;
+    __device__ Weight(float top_, double inv_t) : top(top_) {
+        c = inv_t * 1.4426950408889634;
+        low = fmaxf((float)((double)top - 2000.0 / c), -0x1.fffffep127f);
+    }
+    __device__ double operator()(float v) const {
+        const double w = top == INFINITY ? 1.0 : exp2_of(((double)fmaxf(v, low) - (double)top) * c);
+        return v > (top == INFINITY ? 0x1.fffffep127f : -INFINITY) ? w : 0.0;      // false for NaN as well
+    }
+};
 
 struct Top { float v; int i; };
 __device__ __forceinline__ void take(Top& a, float v, int i) {
@@ -76,8 +82,8 @@ __device__ __forceinline__ double block_sum(double v, double* part) {
 // of a chunk of a row; top = -inf: nothing takes part
 struct Stat {
     float top;
-    int at;
-    double sum;             // of exp((logit - top) / T); not set for greedy requests
+    int at;                 // index of it, for greedy requests
+    double sum;             // of exp((logit - top) / T), for the others
 };
 // what verify_masses found out about a request
 struct Decision {
@@ -92,10 +98,11 @@ struct VerifyArgs {
     int chunk, chunks;
     Stat* stats;            // [2][rows][chunks]
     Decision* decisions;    // [n]
-    double2* masses;        // [n][chunks] of (max(p - q, 0), p)
+    int picks;              // chunks of PICK
+    double2* masses;        // [n][picks] of (max(p - q, 0), p)
 };
 
-__device__ __forceinline__ double inverse(float t) { return t > 0.f ? 1.0 / (double)fminf(t, 0x1.fffffep127f) : 0.0; }       // 0: greedy
+__device__ __forceinline__ double inverse(float t) { return t > 0.f ? 1.0 / (double)fminf(t, 1e30f) : 0.0; }       // 0: greedy
 
 template <class T> struct Eight;
 // 8 logits; rows start anywhere, the hardware takes such loads
@@ -120,7 +127,7 @@ template <class T, int E>
 __global__ __launch_bounds__(THREADS) void verify_stats(const VerifyArgs a) {
     const Verify& v = a.v;
     __shared__ double sums[WAVES];
-    __shared__ Top tops[WAVES];
+    __shared__ float tops[WAVES];
     __shared__ int counts[WAVES];
     const int tid = threadIdx.x, row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks, side = blockIdx.y;
     // the request that the row belongs to: the last that starts at or before it
@@ -148,31 +155,51 @@ __global__ __launch_bounds__(THREADS) void verify_stats(const VerifyArgs a) {
     // the elements that are no whole piece of 8: at most 7, one a thread
     const int tail = n & ~7;
     const float last = tail + tid < n ? logit((float)from[tail + tid]) : -INFINITY;
-    Top top{last, tail + tid};
+    float best = last;
 #pragma unroll
-    for (int j = 0; j < E / 8; ++j) {
-        const int i = (j * THREADS + tid) * 8;
-        if (i + 8 > n) break;
+    for (int j = 0; j < E / 8; ++j)
+        if ((j * THREADS + tid) * 8 + 8 <= n)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) take(top, logit(x[j].at(e)), i + e);
-    }
-    top = wave_top(top);
-    if ((tid & 63) == 0) tops[tid >> 6] = top;
+            for (int e = 0; e < 8; ++e) best = fmaxf(best, x[j].at(e));            // the number, of a NaN and a number
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor(best, o));
+    if ((tid & 63) == 0) tops[tid >> 6] = best;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) take(top, tops[w].v, tops[w].i);
+    for (int w = 0; w < WAVES; ++w) best = fmaxf(best, tops[w]);
     double sum = 0.0;
-    if (inv_t > 0.0 && top.v > -INFINITY) {
-        if (tail + tid < n) sum = weight(last, top.v, inv_t);
+    int at = 0x7fffffff;
+    if (inv_t > 0.0) {
+        if (best > -INFINITY) {
+            const Weight weight(best, inv_t);
+            sum = weight(last);
 #pragma unroll
-        for (int j = 0; j < E / 8; ++j) {
-            if ((j * THREADS + tid) * 8 + 8 > n) break;
+            for (int j = 0; j < E / 8; ++j) {
+                if ((j * THREADS + tid) * 8 + 8 > n) break;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += weight(logit(x[j].at(e)), top.v, inv_t);
+                for (int e = 0; e < 8; ++e) sum += weight(x[j].at(e));
+            }
+            sum = block_sum(sum, sums);
         }
-        sum = block_sum(sum, sums);
+    } else {
+        // greedy: where it is
+        if (last == best) at = tail + tid;
+#pragma unroll
+        for (int j = E / 8 - 1; j >= 0; --j) {
+            const int i = (j * THREADS + tid) * 8;
+            if (i + 8 <= n)
+#pragma unroll
+                for (int e = 7; e >= 0; --e) at = x[j].at(e) == best ? i + e : at;
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) at = min(at, __shfl_xor(at, o));
+        if ((tid & 63) == 0) counts[tid >> 6] = at;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) at = min(at, counts[w]);
+        at += chunk * a.chunk;
     }
-    if (tid == 0) a.stats[((int64_t)side * v.rows + row) * a.chunks + chunk] = Stat{top.v, chunk * a.chunk + top.i, sum};
+    if (tid == 0) a.stats[((int64_t)side * v.rows + row) * a.chunks + chunk] = Stat{best, at, sum};
 }
 
 // a row's chunks joined by one wave
@@ -188,40 +215,65 @@ __device__ __forceinline__ Stat row_stat(const VerifyArgs& a, int side, int row,
     top = wave_top(top);
     double sum = 0.0;
     if (inv_t > 0.0 && top.v > -INFINITY) {
+        const Weight weight(top.v, inv_t);
         for (int c = lane; c < a.chunks; c += 64) {
             if (a.chunks > 64) mine = from[c];
-            if (mine.top > -INFINITY) sum += mine.sum * weight(mine.top, top.v, inv_t);
+            sum += mine.sum * weight(mine.top);
         }
         sum = wave_sum(sum);
     }
     return Stat{top.v, top.i, sum};
 }
 
-// the shares of one token in either model
+// the shares of tokens in either model
 template <class T>
 struct Shares {
     const T *target, *draft;
-    Stat t, d;
-    double inv_t;
-    int drafted;            // the draft itself, where it comes without probabilities
+    Weight p_weight, q_weight;
+    double p_norm, q_norm;  // q_norm = 0: the draft row has no distribution
+    int drafted;            // the draft itself
     bool minus;
-    __device__ double p(int i) const { return weight(logit((float)target[i]), t.top, inv_t) / t.sum; }
-    __device__ double q(int i) const {
-        return !draft ? (double)(i == drafted) : d.top == -INFINITY ? 0.0 : weight(logit((float)draft[i]), d.top, inv_t) / d.sum;
+    __device__ Shares(const VerifyArgs& a, const Decision& d, double inv_t)
+        : p_weight(d.target.top, inv_t), q_weight(d.draft.top > -INFINITY ? d.draft.top : 0.f, inv_t) {
+        target = (const T*)a.v.target + d.row * a.v.ld_target;
+        minus = d.minus >= 0;
+        draft = minus && a.v.draft ? (const T*)a.v.draft + d.minus * a.v.ld_draft : nullptr;
+        p_norm = 1.0 / d.target.sum;
+        q_norm = d.draft.top > -INFINITY ? 1.0 / d.draft.sum : 0.0;
+        drafted = minus ? a.v.tokens[d.minus] : -1;
     }
-    __device__ double rest(int i, double p_) const { return minus ? fmax(p_ - q(i), 0.0) : p_; }
+    __device__ double p(float v) const { return p_weight(v) * p_norm; }
+    __device__ double q(float v, int i) const { return draft ? q_weight(v) * q_norm : (double)(i == drafted); }
 };
+// a thread's 8 tokens of one chunk of PICK: p, and what max(p - q, 0) leaves; i: the first of them
+constexpr int PICK = THREADS * 8;
 template <class T>
-__device__ __forceinline__ Shares<T> shares_of(const VerifyArgs& a, const Decision& d, double inv_t) {
-    Shares<T> s;
-    s.target = (const T*)a.v.target + d.row * a.v.ld_target;
-    s.minus = d.minus >= 0;
-    s.draft = s.minus && a.v.draft ? (const T*)a.v.draft + d.minus * a.v.ld_draft : nullptr;
-    s.t = d.target;
-    s.d = d.draft;
-    s.inv_t = inv_t;
-    s.drafted = s.minus ? a.v.tokens[d.minus] : -1;
-    return s;
+__device__ __forceinline__ int shares_of_chunk(const Shares<T>& s, int chunk, int vocab, double (&p)[8], double (&rest)[8]) {
+    const int i = chunk * PICK + threadIdx.x * 8;
+    float x[8], y[8];
+    if (i + 8 <= vocab) {
+        Eight<T> e;
+        e.load(s.target + i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = e.at(j);
+        if (s.draft) {
+            e.load(s.draft + i);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = e.at(j);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[j] = i + j < vocab ? (float)s.target[i + j] : -INFINITY;
+            y[j] = s.draft && i + j < vocab ? (float)s.draft[i + j] : -INFINITY;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        p[j] = s.p(x[j]);
+        rest[j] = s.minus ? fmax(p[j] - s.q(s.draft ? y[j] : 0.f, i + j), 0.0) : p[j];
+    }
+    return i;
 }
 
 template <class T>
@@ -256,8 +308,8 @@ __global__ __launch_bounds__(THREADS) void verify_masses(const VerifyArgs a) {
             if (greedy) {
                 stands = drafted && !empty && token == d.target.at;
             } else if (valid && !empty) {
-                const Shares<T> s = shares_of<T>(a, d, inv_t);
-                stands = (double)v.u_accept[row + 1] * s.q(token) < s.p(token);
+                const Shares<T> s(a, d, inv_t);
+                stands = (double)v.u_accept[row + 1] * s.q(s.draft ? (float)s.draft[token] : 0.f, token) < s.p((float)s.target[token]);
             } else {
                 stands = false;                           // also the last row of a request, which has no draft behind it
             }
@@ -272,17 +324,17 @@ __global__ __launch_bounds__(THREADS) void verify_masses(const VerifyArgs a) {
     const Decision d = decided;
     if (chunk == 0 && tid == 0) a.decisions[r] = d;
     if (greedy || d.target.top == -INFINITY) return;
-    const Shares<T> s = shares_of<T>(a, d, inv_t);
-    const int i0 = chunk * a.chunk, i1 = min(i0 + a.chunk, v.vocab);
-    double rest = 0.0, all = 0.0;
-    for (int i = i0 + tid; i < i1; i += THREADS) {
-        const double p = s.p(i);
-        all += p;
-        rest += s.rest(i, p);
+    double p[8], rest[8];
+    shares_of_chunk(Shares<T>(a, d, inv_t), chunk, v.vocab, p, rest);
+    double some = 0.0, all = 0.0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        some += rest[j];
+        all += p[j];
     }
-    rest = block_sum(rest, sums);
+    some = block_sum(some, sums);
     all = block_sum(all, sums);
-    if (tid == 0) a.masses[(int64_t)r * a.chunks + chunk] = make_double2(rest, all);
+    if (tid == 0) a.masses[(int64_t)r * a.picks + chunk] = make_double2(some, all);
 }
 
 // sum over the threads before this one; total: over all
@@ -324,26 +376,31 @@ __global__ __launch_bounds__(THREADS) void verify_pick(const VerifyArgs a) {
     const Decision d = a.decisions[r];
     int next = d.token;
     if (inv_t > 0.0 && d.target.top > -INFINITY) {
-        Shares<T> s = shares_of<T>(a, d, inv_t);
-        const double2* masses = a.masses + (int64_t)r * a.chunks;
-        // p where p - q leaves nothing
-        double sum = 0.0;
-        for (int c = tid; c < a.chunks; c += THREADS) sum += masses[c].x;
-        if (!(block_sum(sum, sums) > 0.0)) s.minus = false;
-        // chunks, a run of them per thread
-        const int each = (a.chunks + THREADS - 1) / THREADS, c0 = min(tid * each, a.chunks), c1 = min(c0 + each, a.chunks);
+        Shares<T> s(a, d, inv_t);
+        const double2* masses = a.masses + (int64_t)r * a.picks;
+        // chunks, a run of them per thread; p where p - q leaves nothing
+        const int each = (a.picks + THREADS - 1) / THREADS, c0 = min(tid * each, a.picks), c1 = min(c0 + each, a.picks);
+        double some = 0.0, mine = 0.0, total;
+        for (int c = c0; c < c1; ++c) {
+            const double2 m = masses[c];
+            some += m.x;
+            mine += m.y;
+        }
+        double before = sum_before(some, sums, total);
+        if (!(total > 0.0)) {
+            s.minus = false;
+            before = sum_before(mine, sums, total);
+        }
         auto mass = [&](int c) { return s.minus ? masses[c].x : masses[c].y; };
-        double mine = 0.0, total;
-        for (int c = c0; c < c1; ++c) mine += mass(c);
-        double before = sum_before(mine, sums, total);
         const double goal = (double)v.u_sample[r] * total;
-        if (tid == 0) { found = a.chunks; last = -1; }
+        if (tid == 0) { found = 0x7fffffff; last = -1; }
         __syncthreads();
         {
             double upto = before;
             for (int c = c0; c < c1; ++c) {
-                upto += mass(c);
-                if (mass(c) > 0.0) {
+                const double m = mass(c);
+                upto += m;
+                if (m > 0.0) {
                     atomicMax(&last, c);
                     if (upto > goal) {
                         atomicMin(&found, c);
@@ -353,43 +410,32 @@ __global__ __launch_bounds__(THREADS) void verify_pick(const VerifyArgs a) {
             }
         }
         __syncthreads();
-        const int chunk = found < a.chunks ? found : last;
-        // the sum in front of the chunk, as its thread has it
-        if (chunk >= c0 && chunk < c1) {
+        const int chunk = found < a.picks ? found : last;
+        if (chunk >= c0 && chunk < c1) {                   // the sum in front of the chunk, as its thread has it
             double upto = before;
             for (int c = c0; c < chunk; ++c) upto += mass(c);
             base = upto;
         }
         __syncthreads();
-        if (tid == 0) { found = v.vocab; last = -1; }
-        __syncthreads();
-        // the chunk's tokens, a run of them per thread
-        const int width = (a.chunk + THREADS - 1) / THREADS;
-        const int i0 = min(chunk * a.chunk + tid * width, v.vocab), i1 = min(min(i0 + width, (chunk + 1) * a.chunk), v.vocab);
-        double here = 0.0, unused;
-        for (int i = i0; i < i1; ++i) here += s.rest(i, s.p(i));
-        double upto = base + sum_before(here, sums, unused);
-        // only threads whose run may pass the goal look again, a little more of them than by the sums, which are not exact
-        if (here > 0.0 && upto + here + 1e-9 * total > goal) {
-            for (int i = i0; i < i1; ++i) {
-                const double w = s.rest(i, s.p(i));
-                upto += w;
-                if (w > 0.0 && upto > goal) {
-                    atomicMin(&found, i);
-                    break;
-                }
+        if (tid == 0) { found = 0x7fffffff; last = -1; }
+        double p[8], rest[8], here = 0.0, unused;
+        const int i = shares_of_chunk(s, chunk, v.vocab, p, rest);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) here += rest[j];
+        double upto = sum_before(here, sums, unused) + base;
+        int holds = 0x7fffffff, positive = -1;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            upto += rest[j];
+            if (rest[j] > 0.0) {
+                positive = i + j;
+                if (upto > goal) holds = min(holds, i + j);
             }
         }
+        if (holds < 0x7fffffff) atomicMin(&found, holds);
+        if (positive >= 0) atomicMax(&last, positive);      // where the goal is the whole sum but for its rounding: the last token with a share
         __syncthreads();
-        if (found == v.vocab && here > 0.0) {              // the goal is the whole sum but for its rounding: the last token with a share
-            for (int i = i1 - 1; i >= i0; --i)
-                if (s.rest(i, s.p(i)) > 0.0) {
-                    atomicMax(&last, i);
-                    break;
-                }
-        }
-        __syncthreads();
-        next = found < v.vocab ? found : last;
+        next = found < 0x7fffffff ? found : last;
     }
     for (int i = first + tid; i < end; i += THREADS) v.out[i] = i < d.row ? v.tokens[i + 1] : i == d.row ? next : -1;
     if (tid == 0) {
@@ -401,9 +447,10 @@ __global__ __launch_bounds__(THREADS) void verify_pick(const VerifyArgs a) {
 
 struct Layout {
     int chunk, chunks;
+    int picks;
     size_t stats, decisions, masses;
 };
-// Chunks of 8192 logits, of 4096 or 2048 where that leaves fewer than 1024 workgroups.
+// Chunks of the first launch: 8192 logits, 4096 or 2048 where that leaves fewer than 1024 workgroups.
 Layout layout_of(int n, int rows, int vocab) {
     Layout l;
     l.chunk = 8192;
@@ -411,7 +458,8 @@ Layout layout_of(int n, int rows, int vocab) {
     l.chunks = (vocab + l.chunk - 1) / l.chunk;
     l.stats = 2 * (size_t)rows * l.chunks * sizeof(Stat);
     l.decisions = (size_t)n * sizeof(Decision);
-    l.masses = (size_t)n * l.chunks * sizeof(double2);
+    l.picks = (vocab + PICK - 1) / PICK;
+    l.masses = (size_t)n * l.picks * sizeof(double2);
     return l;
 }
 
@@ -422,6 +470,7 @@ int launch(const Verify& v, void* ws, hipStream_t st) {
     a.v = v;
     a.chunk = l.chunk;
     a.chunks = l.chunks;
+    a.picks = l.picks;
     a.stats = (Stat*)ws;
     a.decisions = (Decision*)((char*)ws + l.stats);
     a.masses = (double2*)((char*)ws + l.stats + l.decisions);
@@ -429,7 +478,7 @@ int launch(const Verify& v, void* ws, hipStream_t st) {
         auto stats = l.chunk == 8192 ? verify_stats<T, 32> : l.chunk == 4096 ? verify_stats<T, 16> : verify_stats<T, 8>;
         hipLaunchKernelGGL(stats, dim3((unsigned)(v.rows * l.chunks), v.draft ? 2 : 1), dim3(THREADS), 0, st, a);
         KVPR_HIP(hipGetLastError());
-        hipLaunchKernelGGL(verify_masses<T>, dim3((unsigned)l.chunks, (unsigned)v.n), dim3(THREADS), 0, st, a);
+        hipLaunchKernelGGL(verify_masses<T>, dim3((unsigned)l.picks, (unsigned)v.n), dim3(THREADS), 0, st, a);
         KVPR_HIP(hipGetLastError());
     }
     hipLaunchKernelGGL(verify_pick<T>, dim3((unsigned)v.n), dim3(THREADS), 0, st, a);
