@@ -3,10 +3,10 @@
 // Three launches over chunks of the vocabulary, since the order of a request's steps leaves one workgroup per request otherwise
 // (five rows of 50272: 226 us in one workgroup):
 //   verify_stats   every row of both models at once: of a chunk the largest logit, its index and the sum of exponentials;
-//   verify_masses  a request's rows joined from their chunks, the run of drafts that stand, and of each chunk of the row behind
-//                  them the sum of max(p - q, 0);
-//   verify_pick    the chunk in which the random number falls, then the token in it.
-// The first reads everything once and is bound by that; the others read one row of each model again, from the caches.
+//   verify_decide  a request's rows joined from their chunks, and the run of drafts that stand;
+//   verify_draw    of each chunk of the row behind them the sum of max(p - q, 0); the last workgroup of a request then finds the chunk in
+//                  which the random number falls, and the token in it.
+// The first reads everything once and is bound by that and its 64-bit arithmetic; the last reads one row of each model again, from the caches.
 // Shares and their sums are held in 64 bits: a uniform number falls between two of some 10^5 borders, and sums in 32 bits would
 // move those by more than a few per mille of the distance of the closer ones.  Partial sums are added in an order that depends on the sizes
 // alone.
@@ -22,35 +22,35 @@ constexpr int THREADS = 256, WAVES = THREADS / 64;
 // a logit that takes part; NaN counts as -inf
 __device__ __forceinline__ float logit(float v) { return v == v ? v : -INFINITY; }
 
-// 2^t for t <= 0: t = k + f with |f| <= 1/2 (adding 1.5 2^52 leaves k in the low word), the polynomial of degree 9 that meets 2^f in the 10
-// Chebyshev points of that interval (off by 2 10^-14 at most), ldexp.  16 instructions of 64 bits where the library's exp and the steps
-// around it take 40: those bound the reading of the logits.
+// 2^t for -1100 <= t <= 0, subnormal numbers among them: t = k + f with |f| <= 1/2 (adding 1.5 2^52 leaves k in the low word), the polynomial of degree 8 that meets 2^f
+// in the 9 Chebyshev points of that interval (off by 1.1 10^-12 at most, in turns above and below), ldexp.  14 instructions of
+// 64 bits, which bound the reading of the logits (they take 8 cycles each), where the library's exp and the steps around it take 40.
 __device__ __forceinline__ double exp2_of(double t) {
     const double big = 6755399441055744.0, kd = t + big, f = t - (kd - big);
-    double p = 1.0212097549811005e-07;
-    p = fma(p, f, 1.3259945262689143e-06);
-    p = fma(p, f, 1.5252640059770786e-05);
-    p = fma(p, f, 0.00015403432339553542);
-    p = fma(p, f, 0.001333355825801874);
-    p = fma(p, f, 0.009618129195951041);
-    p = fma(p, f, 0.05550410866428854);
-    p = fma(p, f, 0.24022650695631514);
-    p = fma(p, f, 0.6931471805599526);
-    p = fma(p, f, 1.000000000000014);
+    double p = 1.325497460306718e-06;
+    p = fma(p, f, 1.531007807039615e-05);
+    p = fma(p, f, 0.00015403457039410448);
+    p = fma(p, f, 0.0013333450573018062);
+    p = fma(p, f, 0.009618129157656703);
+    p = fma(p, f, 0.055504109412010456);
+    p = fma(p, f, 0.24022650695821055);
+    p = fma(p, f, 0.6931471805459343);
+    p = fma(p, f, 0.9999999999999997);
     return __builtin_ldexp(p, __double2loint(kd));
 }
 
 // exp((v - top) / T) of one row; with an infinite top 1 where the logit is infinite too and 0 elsewhere
 struct Weight {
-    float top, low;                 // low: logits that far down have weight 0 whatever they are
+    float top, low;                 // low: logits so far down, and NaN, have weight 0 (below 2^-1075)
     double c;
     __device__ Weight(float top_, double inv_t) : top(top_) {
         c = inv_t * 1.4426950408889634;
-        low = fmaxf((float)((double)top - 2000.0 / c), -0x1.fffffep127f);
+        low = top == INFINITY ? 0x1.fffffep127f : (float)((double)top - 1076.0 / c);
+        if (low == top) low = nextafterf(top, -INFINITY);       // 1076 / c less than half a step of the type
     }
     __device__ double operator()(float v) const {
-        const double w = top == INFINITY ? 1.0 : exp2_of(((double)fmaxf(v, low) - (double)top) * c);
-        return v > (top == INFINITY ? 0x1.fffffep127f : -INFINITY) ? w : 0.0;      // false for NaN as well
+        const double w = top == INFINITY ? 1.0 : exp2_of(((double)v - (double)top) * c);
+        return v > low ? w : 0.0;
     }
 };
 
@@ -85,12 +85,14 @@ struct Stat {
     int at;                 // index of it, for greedy requests
     double sum;             // of exp((logit - top) / T), for the others
 };
-// what verify_masses found out about a request
+// what verify_decide found out about a request whose next token is drawn
 struct Decision {
-    int row, token;         // the row that the next token comes from; greedy: the token
-    int minus;              // draft row to be taken off (row + 1), or -1
-    int pad;
-    Stat target, draft;
+    int first, end, row;    // its rows, and the one that the next token comes from; row = -1: nothing is left to do
+    int drafted;            // the draft that did not stand, to be taken off, or -1
+    float target_top, draft_top;
+    float goal;             // u_sample
+    unsigned arrived;       // workgroups of verify_draw that are done
+    double inv_t, p_norm, q_norm;       // 1 / sums; q_norm = 0: the draft row has no distribution
 };
 
 struct VerifyArgs {
@@ -99,7 +101,7 @@ struct VerifyArgs {
     Stat* stats;            // [2][rows][chunks]
     Decision* decisions;    // [n]
     int picks;              // chunks of PICK
-    double2* masses;        // [n][picks] of (max(p - q, 0), p)
+    double* masses;         // [n][picks] of max(p - q, 0)
 };
 
 __device__ __forceinline__ double inverse(float t) { return t > 0.f ? 1.0 / (double)fminf(t, 1e30f) : 0.0; }       // 0: greedy
@@ -230,25 +232,23 @@ template <class T>
 struct Shares {
     const T *target, *draft;
     Weight p_weight, q_weight;
-    double p_norm, q_norm;  // q_norm = 0: the draft row has no distribution
-    int drafted;            // the draft itself
-    bool minus;
-    __device__ Shares(const VerifyArgs& a, const Decision& d, double inv_t)
-        : p_weight(d.target.top, inv_t), q_weight(d.draft.top > -INFINITY ? d.draft.top : 0.f, inv_t) {
+    double p_norm, q_norm;
+    int drafted;
+    __device__ Shares(const VerifyArgs& a, const Decision& d)
+        : p_weight(d.target_top, d.inv_t), q_weight(d.draft_top > -INFINITY ? d.draft_top : 0.f, d.inv_t) {
         target = (const T*)a.v.target + d.row * a.v.ld_target;
-        minus = d.minus >= 0;
-        draft = minus && a.v.draft ? (const T*)a.v.draft + d.minus * a.v.ld_draft : nullptr;
-        p_norm = 1.0 / d.target.sum;
-        q_norm = d.draft.top > -INFINITY ? 1.0 / d.draft.sum : 0.0;
-        drafted = minus ? a.v.tokens[d.minus] : -1;
+        drafted = d.drafted;
+        draft = drafted >= 0 && a.v.draft ? (const T*)a.v.draft + (d.row + 1) * a.v.ld_draft : nullptr;
+        p_norm = d.p_norm;
+        q_norm = d.q_norm;
     }
     __device__ double p(float v) const { return p_weight(v) * p_norm; }
     __device__ double q(float v, int i) const { return draft ? q_weight(v) * q_norm : (double)(i == drafted); }
 };
-// a thread's 8 tokens of one chunk of PICK: p, and what max(p - q, 0) leaves; i: the first of them
+// max(p - q, 0), or p behind the last draft, of a thread's 8 tokens of one chunk of PICK; gives the first of them
 constexpr int PICK = THREADS * 8;
 template <class T>
-__device__ __forceinline__ int shares_of_chunk(const Shares<T>& s, int chunk, int vocab, double (&p)[8], double (&rest)[8]) {
+__device__ __forceinline__ int shares_of_chunk(const Shares<T>& s, int chunk, int vocab, double (&rest)[8]) {
     const int i = chunk * PICK + threadIdx.x * 8;
     float x[8], y[8];
     if (i + 8 <= vocab) {
@@ -270,45 +270,48 @@ __device__ __forceinline__ int shares_of_chunk(const Shares<T>& s, int chunk, in
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        p[j] = s.p(x[j]);
-        rest[j] = s.minus ? fmax(p[j] - s.q(s.draft ? y[j] : 0.f, i + j), 0.0) : p[j];
+        rest[j] = s.p(x[j]);
+        if (s.drafted >= 0) rest[j] = fmax(rest[j] - s.q(s.draft ? y[j] : 0.f, i + j), 0.0);
     }
     return i;
 }
 
+// One workgroup per request: its rows joined, a wave per row and four rows at a time, up to the first draft that does not stand.
 template <class T>
-__global__ __launch_bounds__(THREADS) void verify_masses(const VerifyArgs a) {
+__global__ __launch_bounds__(THREADS) void verify_decide(const VerifyArgs a) {
     const Verify& v = a.v;
-    __shared__ int stop;
-    __shared__ double sums[WAVES];
-    __shared__ Decision decided;
-    const int tid = threadIdx.x, wave = tid >> 6, chunk = blockIdx.x, r = blockIdx.y;
+    __shared__ int stop, best;
+    const int tid = threadIdx.x, wave = tid >> 6, r = blockIdx.x;
     const int first = max(v.row_start[r], 0), end = min(v.row_start[r + 1], v.rows);
-    if (first >= end) return;
     const double inv_t = inverse(v.temperature[r]);
     const bool greedy = inv_t == 0.0;
-    // a wave per row, four rows at a time, up to the first draft that does not stand
-    int at = first;
-    for (;; at += WAVES) {
+    if (first >= end) {
+        if (tid == 0) {
+            v.kept[r] = 0;
+            if (v.len_out) v.len_out[r] = v.len_in[r];
+            a.decisions[r].row = -1;
+        }
+        return;
+    }
+    for (int at = first;; at += WAVES) {
         if (tid == 0) stop = end;
         __syncthreads();
         const int row = at + wave;
-        Decision d;
-        bool stands = true;
+        Decision d{};
+        bool stands = true, empty = false;
+        int token = -1, top_at = -1;
         if (row < end) {
-            const bool drafted = row + 1 < end;
-            const int token = drafted ? v.tokens[row + 1] : -1;
+            token = row + 1 < end ? v.tokens[row + 1] : -1;
             const bool valid = token >= 0 && token < v.vocab;
-            d.row = row;
-            d.minus = valid && !greedy ? row + 1 : -1;
-            d.target = row_stat(a, 0, row, inv_t);
-            d.draft = valid && v.draft && !greedy ? row_stat(a, 1, row + 1, inv_t) : Stat{-INFINITY, 0, 0.0};
-            const bool empty = d.target.top == -INFINITY;
-            d.token = empty ? -1 : d.target.at;
+            const Stat t = row_stat(a, 0, row, inv_t);
+            const Stat q = valid && v.draft && !greedy ? row_stat(a, 1, row + 1, inv_t) : Stat{-INFINITY, 0, 0.0};
+            empty = t.top == -INFINITY;
+            top_at = empty ? -1 : t.at;
+            d = Decision{first, end, row, valid ? token : -1, t.top, q.top, v.u_sample[r], 0u, inv_t, 1.0 / t.sum, q.top > -INFINITY ? 1.0 / q.sum : 0.0};
             if (greedy) {
-                stands = drafted && !empty && token == d.target.at;
+                stands = row + 1 < end && !empty && token == t.at;
             } else if (valid && !empty) {
-                const Shares<T> s(a, d, inv_t);
+                const Shares<T> s(a, d);
                 stands = (double)v.u_accept[row + 1] * s.q(s.draft ? (float)s.draft[token] : 0.f, token) < s.p((float)s.target[token]);
             } else {
                 stands = false;                           // also the last row of a request, which has no draft behind it
@@ -316,25 +319,20 @@ __global__ __launch_bounds__(THREADS) void verify_masses(const VerifyArgs a) {
             if (!stands && (tid & 63) == 0) atomicMin(&stop, row);
         }
         __syncthreads();
-        if (row < end && row == stop && (tid & 63) == 0) decided = d;
+        if (row < end && row == stop && (tid & 63) == 0) {
+            best = top_at;
+            const int gained = row - first + 1;
+            v.kept[r] = gained;
+            if (v.len_out) v.len_out[r] = v.len_in[r] + gained;
+            if (greedy || empty) d.row = -1;
+            a.decisions[r] = d;
+        }
         __syncthreads();
         if (stop < end) break;
         __syncthreads();
     }
-    const Decision d = decided;
-    if (chunk == 0 && tid == 0) a.decisions[r] = d;
-    if (greedy || d.target.top == -INFINITY) return;
-    double p[8], rest[8];
-    shares_of_chunk(Shares<T>(a, d, inv_t), chunk, v.vocab, p, rest);
-    double some = 0.0, all = 0.0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        some += rest[j];
-        all += p[j];
-    }
-    some = block_sum(some, sums);
-    all = block_sum(all, sums);
-    if (tid == 0) a.masses[(int64_t)r * a.picks + chunk] = make_double2(some, all);
+    // the tokens; one that is drawn is put in its place by verify_draw
+    for (int i = first + tid; i < end; i += THREADS) v.out[i] = i < stop ? v.tokens[i + 1] : i == stop ? best : -1;
 }
 
 // sum over the threads before this one; total: over all
@@ -358,91 +356,106 @@ __device__ __forceinline__ double sum_before(double v, double* part, double& tot
     return before + s - v;
 }
 
+// What goes from workgroup to workgroup of one launch is stored and loaded past the L2 of either's XCD.
+__device__ __forceinline__ void put(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ double get(const double* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// The mass of every chunk of the row that the next token comes from; the workgroup of a request that is done last finds the chunk in which the
+// random number falls, and the token in it.
 template <class T>
-__global__ __launch_bounds__(THREADS) void verify_pick(const VerifyArgs a) {
+__global__ __launch_bounds__(THREADS) void verify_draw(const VerifyArgs a) {
     const Verify& v = a.v;
     __shared__ double sums[WAVES], base;
     __shared__ int found, last;
-    const int tid = threadIdx.x, r = blockIdx.x;
-    const int first = max(v.row_start[r], 0), end = min(v.row_start[r + 1], v.rows);
-    if (first >= end) {
-        if (tid == 0) {
-            v.kept[r] = 0;
-            if (v.len_out) v.len_out[r] = v.len_in[r];
-        }
-        return;
-    }
-    const double inv_t = inverse(v.temperature[r]);
+    const int tid = threadIdx.x, r = blockIdx.y;
     const Decision d = a.decisions[r];
-    int next = d.token;
-    if (inv_t > 0.0 && d.target.top > -INFINITY) {
-        Shares<T> s(a, d, inv_t);
-        const double2* masses = a.masses + (int64_t)r * a.picks;
-        // chunks, a run of them per thread; p where p - q leaves nothing
-        const int each = (a.picks + THREADS - 1) / THREADS, c0 = min(tid * each, a.picks), c1 = min(c0 + each, a.picks);
-        double some = 0.0, mine = 0.0, total;
+    if (d.row < 0) return;
+    Shares<T> s(a, d);
+    double* masses = a.masses + (int64_t)r * a.picks;
+    double rest[8], mine = 0.0, total;
+    shares_of_chunk(s, blockIdx.x, v.vocab, rest);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mine += rest[j];
+    mine = wave_sum(mine);
+    if ((tid & 63) == 0) sums[tid >> 6] = mine;
+    __syncthreads();
+    if (tid == 0) {
+        put(masses + blockIdx.x, (sums[0] + sums[1]) + (sums[2] + sums[3]));
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");            // waits for the store
+        last = (int)__hip_atomic_fetch_add(&a.decisions[r].arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (last != a.picks - 1) return;
+    // chunks, a run of them per thread
+    const int each = (a.picks + THREADS - 1) / THREADS, c0 = min(tid * each, a.picks), c1 = min(c0 + each, a.picks);
+    mine = 0.0;
+    for (int c = c0; c < c1; ++c) mine += get(masses + c);
+    double before = sum_before(mine, sums, total);
+    if (!(total > 0.0)) {
+        // p - q leaves nothing: p itself, whose chunks are summed here, as this is not met but for equal distributions
+        s.drafted = -1;
+        s.draft = nullptr;
+        for (int c = 0; c < a.picks; ++c) {
+            shares_of_chunk(s, c, v.vocab, rest);
+            double here = 0.0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) here += rest[j];
+            here = block_sum(here, sums);
+            if (c >= c0 && c < c1) {
+                put(masses + c, here);
+                mine += here;
+            }
+        }
+        before = sum_before(mine, sums, total);
+    }
+    const double goal = (double)d.goal * total;
+    if (tid == 0) { found = 0x7fffffff; last = -1; }
+    __syncthreads();
+    double upto = before;
+    if (mine > 0.0) {
+        // the thread's first chunk that passes the goal, or its last one with a share
+        int here = -1, passes = 0x7fffffff;
         for (int c = c0; c < c1; ++c) {
-            const double2 m = masses[c];
-            some += m.x;
-            mine += m.y;
-        }
-        double before = sum_before(some, sums, total);
-        if (!(total > 0.0)) {
-            s.minus = false;
-            before = sum_before(mine, sums, total);
-        }
-        auto mass = [&](int c) { return s.minus ? masses[c].x : masses[c].y; };
-        const double goal = (double)v.u_sample[r] * total;
-        if (tid == 0) { found = 0x7fffffff; last = -1; }
-        __syncthreads();
-        {
-            double upto = before;
-            for (int c = c0; c < c1; ++c) {
-                const double m = mass(c);
-                upto += m;
-                if (m > 0.0) {
-                    atomicMax(&last, c);
-                    if (upto > goal) {
-                        atomicMin(&found, c);
-                        break;
-                    }
+            const double m = each == 1 ? mine : get(masses + c);
+            upto += m;
+            if (m > 0.0) {
+                here = c;
+                if (upto > goal) {
+                    passes = c;
+                    break;
                 }
             }
         }
-        __syncthreads();
-        const int chunk = found < a.picks ? found : last;
-        if (chunk >= c0 && chunk < c1) {                   // the sum in front of the chunk, as its thread has it
-            double upto = before;
-            for (int c = c0; c < chunk; ++c) upto += mass(c);
-            base = upto;
-        }
-        __syncthreads();
-        if (tid == 0) { found = 0x7fffffff; last = -1; }
-        double p[8], rest[8], here = 0.0, unused;
-        const int i = shares_of_chunk(s, chunk, v.vocab, p, rest);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) here += rest[j];
-        double upto = sum_before(here, sums, unused) + base;
-        int holds = 0x7fffffff, positive = -1;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            upto += rest[j];
-            if (rest[j] > 0.0) {
-                positive = i + j;
-                if (upto > goal) holds = min(holds, i + j);
-            }
-        }
-        if (holds < 0x7fffffff) atomicMin(&found, holds);
-        if (positive >= 0) atomicMax(&last, positive);      // where the goal is the whole sum but for its rounding: the last token with a share
-        __syncthreads();
-        next = found < 0x7fffffff ? found : last;
+        if (passes < 0x7fffffff) atomicMin(&found, passes);
+        atomicMax(&last, here);
     }
-    for (int i = first + tid; i < end; i += THREADS) v.out[i] = i < d.row ? v.tokens[i + 1] : i == d.row ? next : -1;
-    if (tid == 0) {
-        const int gained = d.row - first + 1;
-        v.kept[r] = gained;
-        if (v.len_out) v.len_out[r] = v.len_in[r] + gained;
+    __syncthreads();
+    const int chunk = found < a.picks ? found : last;
+    if (chunk >= c0 && chunk < c1) {                       // the sum in front of the chunk, as its thread has it
+        upto = before;
+        for (int c = c0; c < chunk; ++c) upto += get(masses + c);
+        base = upto;
     }
+    __syncthreads();
+    if (tid == 0) { found = 0x7fffffff; last = -1; }
+    const int i = shares_of_chunk(s, chunk, v.vocab, rest);
+    double here = 0.0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) here += rest[j];
+    upto = sum_before(here, sums, total) + base;
+    int holds = 0x7fffffff, positive = -1;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        upto += rest[j];
+        if (rest[j] > 0.0) {
+            positive = i + j;
+            if (upto > goal) holds = min(holds, i + j);
+        }
+    }
+    if (holds < 0x7fffffff) atomicMin(&found, holds);
+    if (positive >= 0) atomicMax(&last, positive);          // where the goal is the whole sum but for its rounding: the last token with a share
+    __syncthreads();
+    if (tid == 0) v.out[d.row] = found < 0x7fffffff ? found : last;
 }
 
 struct Layout {
@@ -459,7 +472,7 @@ Layout layout_of(int n, int rows, int vocab) {
     l.stats = 2 * (size_t)rows * l.chunks * sizeof(Stat);
     l.decisions = (size_t)n * sizeof(Decision);
     l.picks = (vocab + PICK - 1) / PICK;
-    l.masses = (size_t)n * l.picks * sizeof(double2);
+    l.masses = (size_t)n * l.picks * sizeof(double);
     return l;
 }
 
@@ -473,16 +486,18 @@ int launch(const Verify& v, void* ws, hipStream_t st) {
     a.picks = l.picks;
     a.stats = (Stat*)ws;
     a.decisions = (Decision*)((char*)ws + l.stats);
-    a.masses = (double2*)((char*)ws + l.stats + l.decisions);
+    a.masses = (double*)((char*)ws + l.stats + l.decisions);
     if (v.rows > 0) {
         auto stats = l.chunk == 8192 ? verify_stats<T, 32> : l.chunk == 4096 ? verify_stats<T, 16> : verify_stats<T, 8>;
         hipLaunchKernelGGL(stats, dim3((unsigned)(v.rows * l.chunks), v.draft ? 2 : 1), dim3(THREADS), 0, st, a);
         KVPR_HIP(hipGetLastError());
-        hipLaunchKernelGGL(verify_masses<T>, dim3((unsigned)l.picks, (unsigned)v.n), dim3(THREADS), 0, st, a);
+    }
+    hipLaunchKernelGGL(verify_decide<T>, dim3((unsigned)v.n), dim3(THREADS), 0, st, a);
+    KVPR_HIP(hipGetLastError());
+    if (v.rows > 0) {
+        hipLaunchKernelGGL(verify_draw<T>, dim3((unsigned)l.picks, (unsigned)v.n), dim3(THREADS), 0, st, a);
         KVPR_HIP(hipGetLastError());
     }
-    hipLaunchKernelGGL(verify_pick<T>, dim3((unsigned)v.n), dim3(THREADS), 0, st, a);
-    KVPR_HIP(hipGetLastError());
     return KVPR_OK;
 }
 
