@@ -405,23 +405,40 @@ def kvpr_decode_attention_mixed(q_dev, kv16_dev, kvq_dev, z_dev, ws_dev, S, spli
 
 
 # ---- ragged batches over a paged 4-bit cache ----
-# Device arguments are checked to be tensors of the stated type on the current device: a host address in a kernel's hands
-# would end the process.
+# Device arguments must be tensors on the current device (a host address in a kernel's hands would end the process), the
+# floating ones of the stated type.  A step of a small batch is a few microseconds on the GPU, so they are looked over without a Python
+# call for each: that took 0.9 us an argument, more than the rest of a plan.
 
-_I32, _F16, _F32 = (torch.int32,), (torch.float16,), (torch.float32,)
-_LOGITS = {KVPR_F16: _F16, KVPR_F32: _F32}
+_data_ptr, _get_device = torch.Tensor.data_ptr, torch.Tensor.get_device
+_FLOATS = {KVPR_F16: torch.float16, KVPR_F32: torch.float32}
 
 
-def _gpu(t, dtypes, name, device):
-    if t is None:
-        return None
-    if isinstance(t, int):
-        return t
-    if not t.is_cuda or t.get_device() != device:
-        raise ValueError(f"{name} must be on the current device cuda:{device}, got {t.device}")
-    if dtypes is not None and t.dtype not in dtypes:
-        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
-    return t.data_ptr()
+def _addresses(*tensors):
+    """Device addresses of tensors, None or ints, and the current device's index in front."""
+    d = torch.cuda.current_device()
+    try:
+        if set(map(_get_device, tensors)) == {d}:
+            return [d, *map(_data_ptr, tensors)]
+    except TypeError:                               # not tensors alone
+        pass
+    out = [d]
+    for i, t in enumerate(tensors):
+        if t is None or isinstance(t, int):
+            out.append(t)
+        elif t.get_device() != d:
+            raise ValueError(f"tensor {i + 1} of the call must be on the current device cuda:{d}, got {t.device}")
+        else:
+            out.append(t.data_ptr())
+    return out
+
+
+def _typed(t, dtype, name):
+    if dtype is not None and getattr(t, "dtype", dtype) is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+
+
+def _current(device, stream):
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else getattr(stream, "cuda_stream", stream)
 
 
 def make_paged_desc(n_heads, n_kv_heads, head_dim, page_size, n_pages, table_width) -> kvpr_paged_desc:
@@ -434,26 +451,24 @@ def kvpr_page_bytes(desc) -> int:
 
 def kvpr_paged_plan(desc, base_len, new_len, n_requests, block_table, held_in, held_out, free_pages, free_count_in, free_count_out,
                     max_rows, row_start, seq_len, slots, positions, refused, stream=None):
-    d = torch.cuda.current_device()
-    _check(lib.kvpr_paged_plan(C.byref(desc), _gpu(base_len, _I32, "base_len", d), _gpu(new_len, _I32, "new_len", d), n_requests,
-                               _gpu(block_table, _I32, "block_table", d), _gpu(held_in, _I32, "held_in", d), _gpu(held_out, _I32, "held_out", d),
-                               _gpu(free_pages, _I32, "free_pages", d), _gpu(free_count_in, _I32, "free_count_in", d),
-                               _gpu(free_count_out, _I32, "free_count_out", d), max_rows, _gpu(row_start, _I32, "row_start", d),
-                               _gpu(seq_len, _I32, "seq_len", d), _gpu(slots, _I32, "slots", d), _gpu(positions, _I32, "positions", d),
-                               _gpu(refused, _I32, "refused", d), _stream(stream)))
+    d, base, new, table, hi, ho, free, ci, co, start, seq, slot, pos, ref = _addresses(
+        base_len, new_len, block_table, held_in, held_out, free_pages, free_count_in, free_count_out, row_start, seq_len, slots, positions, refused)
+    _check(lib.kvpr_paged_plan(C.byref(desc), base, new, n_requests, table, hi, ho, free, ci, co, max_rows, start, seq, slot, pos, ref,
+                               _current(d, stream)))
 
 
 def kvpr_paged_append(desc, qkv_dev, ld, slots, positions, n_rows, rope_table, n_pos, q_out, ldq, pages, stream=None):
-    d = torch.cuda.current_device()
-    _check(lib.kvpr_paged_append(C.byref(desc), _gpu(qkv_dev, _F16, "qkv_dev", d), ld, _gpu(slots, _I32, "slots", d),
-                                 _gpu(positions, _I32, "positions", d), n_rows, _gpu(rope_table, _F32, "rope_table", d), n_pos,
-                                 _gpu(q_out, _F16, "q_out", d), ldq, _gpu(pages, None, "pages", d), _stream(stream)))
+    _typed(qkv_dev, torch.float16, "qkv_dev")
+    _typed(q_out, torch.float16, "q_out")
+    _typed(rope_table, torch.float32, "rope_table")
+    d, qkv, slot, pos, rope, q, pool = _addresses(qkv_dev, slots, positions, rope_table, q_out, pages)
+    _check(lib.kvpr_paged_append(C.byref(desc), qkv, ld, slot, pos, n_rows, rope, n_pos, q, ldq, pool, _current(d, stream)))
 
 
 def kvpr_paged_read(desc, pages, slots, n_rows, kv_dev, ld, stream=None):
-    d = torch.cuda.current_device()
-    _check(lib.kvpr_paged_read(C.byref(desc), _gpu(pages, None, "pages", d), _gpu(slots, _I32, "slots", d), n_rows,
-                               _gpu(kv_dev, _F16, "kv_dev", d), ld, _stream(stream)))
+    _typed(kv_dev, torch.float16, "kv_dev")
+    d, pool, slot, kv = _addresses(pages, slots, kv_dev)
+    _check(lib.kvpr_paged_read(C.byref(desc), pool, slot, n_rows, kv, ld, _current(d, stream)))
 
 
 def kvpr_paged_attention_workspace_bytes(desc, n_requests, n_rows, max_new, max_len) -> int:
@@ -462,11 +477,11 @@ def kvpr_paged_attention_workspace_bytes(desc, n_requests, n_rows, max_new, max_
 
 def kvpr_paged_attention(desc, q_dev, q_type, ldq, pages, block_table, row_start, seq_len, n_requests, n_rows, max_new, max_len, z_dev, ldz,
                          ws_dev, ws_bytes, stream=None):
-    d = torch.cuda.current_device()
-    _check(lib.kvpr_paged_attention(C.byref(desc), _gpu(q_dev, _LOGITS.get(q_type), "q_dev", d), q_type, ldq, _gpu(pages, None, "pages", d),
-                                    _gpu(block_table, _I32, "block_table", d), _gpu(row_start, _I32, "row_start", d),
-                                    _gpu(seq_len, _I32, "seq_len", d), n_requests, n_rows, max_new, max_len, _gpu(z_dev, _F16, "z_dev", d), ldz,
-                                    _gpu(ws_dev, None, "ws_dev", d), ws_bytes, _stream(stream)))
+    _typed(q_dev, _FLOATS.get(q_type), "q_dev")
+    _typed(z_dev, torch.float16, "z_dev")
+    d, q, pool, table, start, seq, z, ws = _addresses(q_dev, pages, block_table, row_start, seq_len, z_dev, ws_dev)
+    _check(lib.kvpr_paged_attention(C.byref(desc), q, q_type, ldq, pool, table, start, seq, n_requests, n_rows, max_new, max_len, z, ldz, ws,
+                                    ws_bytes, _current(d, stream)))
 
 
 def kvpr_verify_workspace_bytes(n_requests, n_rows, vocab) -> int:
@@ -475,11 +490,10 @@ def kvpr_verify_workspace_bytes(n_requests, n_rows, vocab) -> int:
 
 def kvpr_verify_drafts(target_logits, draft_logits, logits_type, ld_target, ld_draft, vocab, tokens, row_start, n_requests, n_rows, temperature,
                        u_accept, u_sample, len_in, len_out, kept, out_tokens, ws_dev, ws_bytes, stream=None):
-    d = torch.cuda.current_device()
-    types = _LOGITS.get(logits_type)
-    _check(lib.kvpr_verify_drafts(_gpu(target_logits, types, "target_logits", d), _gpu(draft_logits, types, "draft_logits", d), logits_type,
-                                  ld_target, ld_draft, vocab, _gpu(tokens, _I32, "tokens", d), _gpu(row_start, _I32, "row_start", d), n_requests,
-                                  n_rows, _gpu(temperature, _F32, "temperature", d), _gpu(u_accept, _F32, "u_accept", d),
-                                  _gpu(u_sample, _F32, "u_sample", d), _gpu(len_in, _I32, "len_in", d), _gpu(len_out, _I32, "len_out", d),
-                                  _gpu(kept, _I32, "kept", d), _gpu(out_tokens, _I32, "out_tokens", d), _gpu(ws_dev, None, "ws_dev", d), ws_bytes,
-                                  _stream(stream)))
+    dtype = _FLOATS.get(logits_type)
+    _typed(target_logits, dtype, "target_logits")
+    _typed(draft_logits, dtype, "draft_logits")
+    d, target, draft, tok, start, temp, ua, us, li, lo, kp, out, ws = _addresses(
+        target_logits, draft_logits, tokens, row_start, temperature, u_accept, u_sample, len_in, len_out, kept, out_tokens, ws_dev)
+    _check(lib.kvpr_verify_drafts(target, draft, logits_type, ld_target, ld_draft, vocab, tok, start, n_requests, n_rows, temp, ua, us, li, lo,
+                                  kp, out, ws, ws_bytes, _current(d, stream)))

@@ -109,3 +109,8 @@ def test_tensors_of_the_wrong_kind(k):
         args[at] = host
         with pytest.raises(ValueError, match="current device"):
             fn(*args, stream=0)
+    for name, at in (("append", 1), ("append", 8), ("append", 6), ("read", 4), ("attention", 1), ("attention", 12), ("verify", 0), ("verify", 1)):
+        fn, args = _calls(k, desc)[name]
+        args[at] = torch.zeros(16, dtype=torch.int32)
+        with pytest.raises(TypeError, match="must be torch.float"):
+            fn(*args, stream=0)
