@@ -4,6 +4,11 @@
 // head with element i + d / 2), q goes out as float16, k and v are packed by the codec of the compressed store into the token's
 // slot.  The rotation is evaluated in 64 bits and rounded to float16 once: a code depends on the float16 value, so an ulp
 // would now and then move a value by a whole step of the codec.
+//
+// Both kernels stream.  A lane has 8 columns of a head (16 bytes in, one word of codes out), a wave four rows of one head (d = 128) or
+// two (d = 64): the codes of a row's keys are 64 bytes in a row, those of four rows 256.  Values lie with the bytes of four positions side by
+// side.  Where four rows are the four positions of such a quad (a prompt's rows are), the wave that has the first of them turns
+// their bytes over between its lanes and stores whole words; other rows store bytes.
 #include "int4_codec.h"
 #include "paged.h"
 
@@ -20,86 +25,197 @@ __device__ __forceinline__ _Float16 to_half(double x) {
     return (_Float16)__int_as_float(bits);
 }
 
-// One wave per head of a token: lane i holds element i and, for d = 128, element i + 64 too.
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef uint32_t word2 __attribute__((ext_vector_type(2)));
+constexpr int WAVES = 4;
+
+// 8 columns rotated: lane j's element e goes with that of the lane half a head further
 template <int D>
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedShape s, const _Float16* __restrict__ qkv, int64_t ld,
-                                                           const int32_t* __restrict__ slots, const int32_t* __restrict__ positions,
-                                                           const float2* __restrict__ rope, int n_pos, _Float16* __restrict__ q_out,
-                                                           int64_t ldq, uint8_t* __restrict__ pages) {
-    constexpr int E = D / 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x;
-    const int slot = slots[row];
-    const int position = rope ? positions[row] : 0;
-    if (rope && (position < 0 || position >= n_pos)) return;
-    const bool kept = slot >= 0 && slot < s.n_pages * s.page;
-    const int page = kept ? slot >> s.page_log2 : 0, t = kept ? slot & (s.page - 1) : 0;
-    for (int head = (q_out ? 0 : s.heads) + wave; head < s.heads + 2 * s.kv_heads; head += 4) {
-        const bool is_q = head < s.heads, is_k = !is_q && head < s.heads + s.kv_heads;
-        const _Float16* src = qkv + (int64_t)row * ld + (int64_t)head * D;
-        _Float16 x[E];
+__device__ __forceinline__ half8 rotate(half8 x, const float2* __restrict__ rope, int64_t position, int j) {
+    constexpr int LANES = D / 8;
+    union { half8 h; int w[4]; } mine, other;
+    mine.h = x;
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = src[lane + 64 * e];
-        if (rope && (is_q || is_k)) {
-            const int i = lane & (D / 2 - 1);
-            const float2 cs = rope[(int64_t)position * (D / 2) + i];
-            if constexpr (D == 128) {
-                const double a = (double)(float)x[0], b = (double)(float)x[1];
-                x[0] = to_half(a * cs.x - b * cs.y);
-                x[1] = to_half(b * cs.x + a * cs.y);
-            } else {
-                const float other = __shfl_xor((float)x[0], 32);
-                const double a = (double)(float)x[0], b = (double)other;
-                x[0] = to_half(lane < 32 ? a * cs.x - b * cs.y : a * cs.x + b * cs.y);
+    for (int i = 0; i < 4; ++i) other.w[i] = __shfl_xor(mine.w[i], LANES / 2);
+    const float4* cs = reinterpret_cast<const float4*>(rope + position * (D / 2) + (j & (LANES / 2 - 1)) * 8);
+    const double side = j < LANES / 2 ? -1.0 : 1.0;
+    half8 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 t = cs[i];
+        out[2 * i] = to_half(fma(side * (double)(float)other.h[2 * i], (double)t.y, (double)(float)x[2 * i] * (double)t.x));
+        out[2 * i + 1] = to_half(fma(side * (double)(float)other.h[2 * i + 1], (double)t.w, (double)(float)x[2 * i + 1] * (double)t.z));
+    }
+    return out;
+}
+
+template <int CTRL>
+__device__ __forceinline__ float across(float v) {       // the value of another lane of the same row of 16
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+
+struct Packed { uint32_t codes, pair; };
+// codes of a lane's 8 columns, and the (scale, minimum) of the group of 64, which 8 lanes share
+__device__ __forceinline__ Packed pack(half8 x) {
+    float mn = (float)x[0], mx = mn;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+        mn = fminf(mn, (float)x[i]);
+        mx = fmaxf(mx, (float)x[i]);
+    }
+    mn = fminf(mn, across<0xB1>(mn)); mx = fmaxf(mx, across<0xB1>(mx));          // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror
+    mn = fminf(mn, across<0x4E>(mn)); mx = fmaxf(mx, across<0x4E>(mx));
+    mn = fminf(mn, across<0x141>(mn)); mx = fmaxf(mx, across<0x141>(mx));
+    const _Float16 scale16 = int4_scale(mn, mx);
+    const float scale = (float)scale16, r = __builtin_amdgcn_rcpf(scale);
+    float part[2];                                       // four codes each as one number below 2^16
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float c[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = int4_code((float)x[4 * i + e], scale, mn, r);
+        part[i] = fmaf(fmaf(c[3], 16.f, c[2]), 256.f, fmaf(c[1], 16.f, c[0]));
+    }
+    union { _Float16 h[2]; uint32_t u; } pair;
+    pair.h[0] = scale16;
+    pair.h[1] = (_Float16)mn;
+    return Packed{scale > 0.f ? (uint32_t)part[0] | (uint32_t)part[1] << 16 : 0u, pair.u};
+}
+
+// Byte i of the words of the four lanes l, l ^ 16, l ^ 32, l ^ 48 (in the order of lane >> 4) for lane >> 4 == i.
+__device__ __forceinline__ uint32_t turn_over(uint32_t v) {
+    const auto half = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    const auto a = __builtin_amdgcn_permlane16_swap(half[0], half[0], false, false), b = __builtin_amdgcn_permlane16_swap(half[1], half[1], false, false);
+    const uint32_t i = (threadIdx.x & 63) >> 4, pick = i | (4 + i) << 8 | 0x0C0C0000u;      // 0x0C: a zero byte
+    return __builtin_amdgcn_perm(a[1], a[0], pick) | __builtin_amdgcn_perm(b[1], b[0], pick) << 16;
+}
+
+template <int D, int HEADS>             // heads that a wave has, one behind the other
+__global__ __launch_bounds__(WAVES * 64) void paged_append_kernel(PagedShape s, const _Float16* __restrict__ qkv, int64_t ld,
+                                                                  const int32_t* __restrict__ slots, const int32_t* __restrict__ positions, int rows,
+                                                                  const float2* __restrict__ rope, int n_pos, _Float16* __restrict__ q_out,
+                                                                  int64_t ldq, uint8_t* __restrict__ pages) {
+    constexpr int LANES = D / 8, SIDE = 16 / LANES, NG = D / 64;       // lanes of a head, heads side by side
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane >> 4, j = lane & (LANES - 1);
+    const int row0 = blockIdx.x * 4, row = row0 + sub;
+    const int pool = s.n_pages * s.page;
+    // the slot of a row as far as it is kept
+    auto slot_of = [&](int r) {
+        if (r < 0 || r >= rows) return -1;
+        const int slot = slots[r];
+        if (slot < 0 || slot >= pool) return -1;
+        if (rope && (positions[r] < 0 || positions[r] >= n_pos)) return -1;
+        return slot;
+    };
+    // slots of rows row0 - 3 .. row0 + 6, a lane each; of a row r: is it one of four rows that are a quad of positions?
+    const int near = slot_of(lane < 10 ? row0 - 3 + lane : -1);
+    auto quad_of = [&](int r) {          // first row of the quad, or -1
+        const int slot = __shfl(near, r - row0 + 3), first = r - (slot & 3);
+        bool whole = slot >= 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) whole &= __shfl(near, min(max(first + i - row0 + 3, 0), 9)) == (slot & ~3) + i;
+        return whole ? first : -1;
+    };
+    const int slot = __shfl(near, sub + 3), quad = quad_of(row);
+    // the quad that starts here: at most one
+    const bool starts = quad == row && row < row0 + 4;
+    const uint64_t who = __ballot(starts);
+    const int lead = who ? row0 + (__builtin_ctzll(who) >> 4) : -1;     // its first row
+    const bool alone = slot >= 0 && quad < 0;
+    const int lead_slot = lead >= 0 ? __shfl(near, lead - row0 + 3) : 0;
+    const bool there = row < rows, turned = there && (!rope || (positions[row] >= 0 && positions[row] < n_pos));
+    const int64_t position = rope && turned ? positions[row] : 0;
+    const int q_heads = q_out ? s.heads : 0, units = (q_heads + 2 * s.kv_heads + SIDE - 1) / SIDE;
+    const int unit0 = (blockIdx.y * WAVES + wave) * HEADS;
+    for (int unit = unit0; unit < min(unit0 + HEADS, units); ++unit) {
+        const int h = unit * SIDE + (SIDE > 1 ? (lane >> 3) & 1 : 0);
+        const bool exists = h < q_heads + 2 * s.kv_heads;
+        const bool is_q = h < q_heads, is_k = !is_q && h < q_heads + s.kv_heads;
+        const int head = h - (is_q ? 0 : is_k ? q_heads : q_heads + s.kv_heads);
+        const int64_t column = (int64_t)(is_q ? head : is_k ? s.heads + head : s.heads + s.kv_heads + head) * D + j * 8;
+        auto load = [&](int r, bool ok) { return ok ? *reinterpret_cast<const half8*>(qkv + r * ld + column) : half8{}; };
+        if (is_q || is_k) {
+            half8 x = load(row, there && exists);
+            if (rope) x = rotate<D>(x, rope, position, j);
+            if (is_q) {
+                if (turned) *reinterpret_cast<half8*>(q_out + row * ldq + (int64_t)head * D + j * 8) = x;
+                continue;
             }
-        }
-        if (is_q) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) q_out[(int64_t)row * ldq + (int64_t)head * D + lane + 64 * e] = x[e];
+            const Packed p = pack(x);
+            if (slot < 0 || !exists) continue;
+            const int t = slot & (s.page - 1);
+            uint8_t* block = pages + (int64_t)(slot >> s.page_log2) * s.page_bytes() + (int64_t)head * s.block_bytes();
+            *reinterpret_cast<uint32_t*>(block + t * (D / 2) + key_place<D>(4 * j)) = p.codes;
+            if ((j & 7) == 0) *reinterpret_cast<uint32_t*>(block + s.page * D + (t * NG + (j >> 3)) * 4) = p.pair;
             continue;
         }
-        if (!kept) continue;
-        uint8_t* block = pages + (int64_t)page * s.page_bytes() + (int64_t)(is_k ? head - s.heads : head - s.heads - s.kv_heads) * s.block_bytes();
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            float mn = (float)x[e], mx = mn;
-            for (int o = 32; o > 0; o >>= 1) {
-                mn = fminf(mn, __shfl_xor(mn, o));
-                mx = fmaxf(mx, __shfl_xor(mx, o));
+        // values: the quad that starts here, whose last rows may be the next wave's, then rows that are in none
+        if (lead >= 0) {
+            const Packed p = pack(load(lead + sub, exists));
+            const uint32_t word = turn_over(p.codes);
+            const int t = (lead_slot & (s.page - 1)) + sub;
+            uint8_t* block = pages + (int64_t)(lead_slot >> s.page_log2) * s.page_bytes() + (int64_t)head * s.block_bytes();
+            if (exists) {
+                *reinterpret_cast<uint32_t*>(block + s.page * (D / 2) + (t >> 2) * (2 * D) + value_place<D>(4 * j + sub) * 4) = word;
+                if ((j & 7) == 0) *reinterpret_cast<uint32_t*>(block + s.page * D + s.page * (NG * 4) + (t * NG + (j >> 3)) * 4) = p.pair;
             }
-            const _Float16 scale16 = int4_scale(mn, mx);
-            const float scale = (float)scale16;
-            const int code = scale > 0.f ? (int)int4_code((float)x[e], scale, mn, __builtin_amdgcn_rcpf(scale)) : 0;
-            const int pair = code | __shfl_xor(code, 1) << 4;
-            const int k = 32 * e + lane / 2;
-            if (!(lane & 1))
-                block[is_k ? t * (D / 2) + key_place<D>(k) : s.page * (D / 2) + (t >> 2) * (2 * D) + value_place<D>(k) * 4 + (t & 3)] = (uint8_t)pair;
-            if (lane == 0) {
-                _Float16* meta = reinterpret_cast<_Float16*>(block + s.page * D + (is_k ? 0 : s.page * (D / 16)) + (t * (D / 64) + e) * 4);
-                meta[0] = scale16;
-                meta[1] = (_Float16)mn;
+        }
+        if (__any(alone)) {
+            const Packed p = pack(load(row, alone && exists));
+            if (alone && exists) {
+                const int t = slot & (s.page - 1);
+                uint8_t* block = pages + (int64_t)(slot >> s.page_log2) * s.page_bytes() + (int64_t)head * s.block_bytes();
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    block[s.page * (D / 2) + (t >> 2) * (2 * D) + value_place<D>(4 * j + i) * 4 + (t & 3)] = (uint8_t)(p.codes >> (8 * i));
+                if ((j & 7) == 0) *reinterpret_cast<uint32_t*>(block + s.page * D + s.page * (NG * 4) + (t * NG + (j >> 3)) * 4) = p.pair;
             }
         }
     }
 }
 
-// One thread per byte of codes: two columns of one head of one row.
+// A lane has 8 columns of a head; of values it reads the four words that hold its bytes beside those of the neighbouring positions, which as
+// a rule other rows of the wave need.
 template <int D>
-__global__ __launch_bounds__(256) void paged_read_kernel(PagedShape s, const uint8_t* __restrict__ pages, const int32_t* __restrict__ slots,
-                                                         _Float16* __restrict__ kv, int64_t ld) {
-    const int row = blockIdx.x, slot = slots[row];
+__global__ __launch_bounds__(WAVES * 64) void paged_read_kernel(PagedShape s, const uint8_t* __restrict__ pages, const int32_t* __restrict__ slots,
+                                                                int rows, _Float16* __restrict__ kv, int64_t ld) {
+    constexpr int LANES = D / 8, SIDE = 16 / LANES, NG = D / 64, U = 2;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane >> 4, j = lane & (LANES - 1);
+    const int row = blockIdx.x * 4 + sub;
+    const int slot = row < rows ? slots[row] : -1;
     if (slot < 0 || slot >= s.n_pages * s.page) return;
-    const int page = slot >> s.page_log2, t = slot & (s.page - 1);
-    const int per_side = s.kv_heads * (D / 2);
-    for (int i = threadIdx.x; i < 2 * per_side; i += 256) {
-        const bool is_k = i < per_side;
-        const int j = is_k ? i : i - per_side, head = j / (D / 2), k = j % (D / 2);
-        const uint8_t* block = pages + (int64_t)page * s.page_bytes() + (int64_t)head * s.block_bytes();
-        const int byte = block[is_k ? t * (D / 2) + key_place<D>(k) : s.page * (D / 2) + (t >> 2) * (2 * D) + value_place<D>(k) * 4 + (t & 3)];
-        const _Float16* meta = reinterpret_cast<const _Float16*>(block + s.page * D + (is_k ? 0 : s.page * (D / 16)) + (t * (D / 64) + k / 32) * 4);
-        const float scale = (float)meta[0], mn = (float)meta[1];
-        _Float16* out = kv + (int64_t)row * ld + 2 * i;
-        out[0] = (_Float16)((float)(byte & 15) * scale + mn);
-        out[1] = (_Float16)((float)(byte >> 4) * scale + mn);
+    const int t = slot & (s.page - 1);
+    const uint8_t* page = pages + (int64_t)(slot >> s.page_log2) * s.page_bytes();
+    uint32_t codes[U], pairs[U];
+    half8* to[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int h = ((blockIdx.y * WAVES + wave) * U + u) * SIDE + (SIDE > 1 ? (lane >> 3) & 1 : 0);
+        to[u] = nullptr;
+        if (h >= 2 * s.kv_heads) break;
+        const bool is_k = h < s.kv_heads;
+        const uint8_t* block = page + (int64_t)(is_k ? h : h - s.kv_heads) * s.block_bytes();
+        if (is_k) {
+            codes[u] = *reinterpret_cast<const uint32_t*>(block + t * (D / 2) + key_place<D>(4 * j));
+        } else {
+            // bytes 4 j, 4 j + 1 lie in neighbouring words, and so do 4 j + 2, 4 j + 3
+            const uint8_t* words = block + s.page * (D / 2) + (t >> 2) * (2 * D);
+            const word2 a = *reinterpret_cast<const word2*>(words + value_place<D>(4 * j) * 4), b = *reinterpret_cast<const word2*>(words + value_place<D>(4 * j + 2) * 4);
+            const int by = 8 * (t & 3);
+            codes[u] = (a[0] >> by & 255u) | (a[1] >> by & 255u) << 8 | (b[0] >> by & 255u) << 16 | (b[1] >> by & 255u) << 24;
+        }
+        pairs[u] = *reinterpret_cast<const uint32_t*>(block + s.page * D + (is_k ? 0 : s.page * (NG * 4)) + (t * NG + (j >> 3)) * 4);
+        to[u] = reinterpret_cast<half8*>(kv + row * ld + (int64_t)h * D + j * 8);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (!to[u]) break;
+        union { uint32_t u; _Float16 h[2]; } pair;
+        pair.u = pairs[u];
+        half8 out;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = (_Float16)((float)(codes[u] >> (4 * i) & 15u) * (float)pair.h[0] + (float)pair.h[1]);
+        *to[u] = out;
     }
 }
 
@@ -107,16 +223,26 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedShape s, const uin
 
 int launch_paged_append(const PagedShape& s, const void* qkv, int64_t ld, const int32_t* slots, const int32_t* positions, int rows,
                         const void* rope, int n_pos, void* q_out, int64_t ldq, void* pages, hipStream_t st) {
-    auto kern = s.d == 128 ? paged_append_kernel<128> : paged_append_kernel<64>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(256), 0, st, s, (const _Float16*)qkv, ld, slots, positions, (const float2*)rope,
-                       n_pos, (_Float16*)q_out, ldq, (uint8_t*)pages);
-    KVPR_HIP(hipGetLastError());
-    return KVPR_OK;
+    const int units = ((q_out ? s.heads : 0) + 2 * s.kv_heads) * s.d / 128 + 1;      // of a wave: one head, two of 64 columns
+    const int64_t quads = ((int64_t)rows + 3) / 4;
+    // Eight heads a wave, whose slots and angles are then looked up once; one where that would leave the GPU's 1024 SIMDs without two waves each
+    const bool many = quads * units >= 8 * 2048;
+    auto launch = [&](auto kern, int heads) -> int {
+        const dim3 grid((unsigned)quads, (unsigned)((units + WAVES * heads - 1) / (WAVES * heads)));
+        hipLaunchKernelGGL(kern, grid, dim3(WAVES * 64), 0, st, s, (const _Float16*)qkv, ld, slots, positions, rows, (const float2*)rope, n_pos,
+                           (_Float16*)q_out, ldq, (uint8_t*)pages);
+        KVPR_HIP(hipGetLastError());
+        return KVPR_OK;
+    };
+    if (s.d == 128) return many ? launch(paged_append_kernel<128, 8>, 8) : launch(paged_append_kernel<128, 1>, 1);
+    return many ? launch(paged_append_kernel<64, 8>, 8) : launch(paged_append_kernel<64, 1>, 1);
 }
 
 int launch_paged_read(const PagedShape& s, const void* pages, const int32_t* slots, int rows, void* kv, int64_t ld, hipStream_t st) {
+    const int units = (2 * s.kv_heads * s.d + 127) / 128;
+    const dim3 grid((unsigned)(((int64_t)rows + 3) / 4), (unsigned)((units + 2 * WAVES - 1) / (2 * WAVES)));
     auto kern = s.d == 128 ? paged_read_kernel<128> : paged_read_kernel<64>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(256), 0, st, s, (const uint8_t*)pages, slots, (_Float16*)kv, ld);
+    hipLaunchKernelGGL(kern, grid, dim3(WAVES * 64), 0, st, s, (const uint8_t*)pages, slots, rows, (_Float16*)kv, ld);
     KVPR_HIP(hipGetLastError());
     return KVPR_OK;
 }
