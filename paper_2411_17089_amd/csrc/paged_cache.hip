@@ -97,8 +97,11 @@ __global__ __launch_bounds__(WAVES * 64) void paged_append_kernel(PagedShape s, 
                                                                   int64_t ldq, uint8_t* __restrict__ pages) {
     constexpr int LANES = D / 8, SIDE = 16 / LANES, NG = D / 64;       // lanes of a head, heads side by side
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane >> 4, j = lane & (LANES - 1);
-    const int row0 = blockIdx.x * 4, row = row0 + sub;
+    // the waves of a workgroup have neighbouring rows of the same heads: pairs of 16 positions are one line of memory (with the waves on
+    // other heads, and the neighbouring rows on another XCD, 8191 rows of 14336 columns took 101 us)
+    const int row0 = (blockIdx.x * WAVES + wave) * 4, row = row0 + sub;
     const int pool = s.n_pages * s.page;
+    if (row0 >= rows) return;
     // the slot of a row as far as it is kept
     auto slot_of = [&](int r) {
         if (r < 0 || r >= rows) return -1;
@@ -126,22 +129,46 @@ __global__ __launch_bounds__(WAVES * 64) void paged_append_kernel(PagedShape s, 
     const bool there = row < rows, turned = there && (!rope || (positions[row] >= 0 && positions[row] < n_pos));
     const int64_t position = rope && turned ? positions[row] : 0;
     const int q_heads = q_out ? s.heads : 0, units = (q_heads + 2 * s.kv_heads + SIDE - 1) / SIDE;
-    const int unit0 = (blockIdx.y * WAVES + wave) * HEADS;
-    for (int unit = unit0; unit < min(unit0 + HEADS, units); ++unit) {
+    const int unit0 = blockIdx.y * HEADS;
+    // what a lane has of a unit
+    struct Part { bool exists, is_q, is_k; int head; int64_t column; };
+    auto part_of = [&](int unit) {
+        Part p;
         const int h = unit * SIDE + (SIDE > 1 ? (lane >> 3) & 1 : 0);
-        const bool exists = h < q_heads + 2 * s.kv_heads;
-        const bool is_q = h < q_heads, is_k = !is_q && h < q_heads + s.kv_heads;
-        const int head = h - (is_q ? 0 : is_k ? q_heads : q_heads + s.kv_heads);
-        const int64_t column = (int64_t)(is_q ? head : is_k ? s.heads + head : s.heads + s.kv_heads + head) * D + j * 8;
-        auto load = [&](int r, bool ok) { return ok ? *reinterpret_cast<const half8*>(qkv + r * ld + column) : half8{}; };
+        p.exists = unit < units && h < q_heads + 2 * s.kv_heads;
+        p.is_q = h < q_heads;
+        p.is_k = !p.is_q && h < q_heads + s.kv_heads;
+        p.head = h - (p.is_q ? 0 : p.is_k ? q_heads : q_heads + s.kv_heads);
+        p.column = (int64_t)(p.is_q ? p.head : p.is_k ? s.heads + p.head : s.heads + s.kv_heads + p.head) * D + j * 8;
+        return p;
+    };
+    auto load = [&](const Part& p, int r, bool ok) {
+        return ok && p.exists ? __builtin_nontemporal_load(reinterpret_cast<const half8*>(qkv + r * ld + p.column)) : half8{};
+    };
+    // of values the rows of the quad that starts here, whose last ones may be the next wave's
+    auto load_unit = [&](const Part& p) {
+        const bool quad_row = !p.is_q && !p.is_k && lead >= 0;
+        return load(p, quad_row ? lead + sub : row, quad_row || there);
+    };
+    // AHEAD units' columns are on their way together (one ahead: 8191 rows of 14336 columns 106 us, bound by the bytes in flight)
+    constexpr int AHEAD = HEADS < 4 ? HEADS : 4;
+    half8 ahead[AHEAD];
+    for (int unit = unit0; unit < min(unit0 + HEADS, units); unit += AHEAD) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) ahead[i] = load_unit(part_of(unit + i));
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+        const Part part = part_of(unit + i);
+        half8 here = ahead[i];
+        const bool exists = part.exists, is_q = part.is_q, is_k = part.is_k;
+        const int head = part.head;
         if (is_q || is_k) {
-            half8 x = load(row, there && exists);
-            if (rope) x = rotate<D>(x, rope, position, j);
+            if (rope) here = rotate<D>(here, rope, position, j);
             if (is_q) {
-                if (turned) *reinterpret_cast<half8*>(q_out + row * ldq + (int64_t)head * D + j * 8) = x;
+                if (turned) *reinterpret_cast<half8*>(q_out + row * ldq + (int64_t)head * D + j * 8) = here;
                 continue;
             }
-            const Packed p = pack(x);
+            const Packed p = pack(here);
             if (slot < 0 || !exists) continue;
             const int t = slot & (s.page - 1);
             uint8_t* block = pages + (int64_t)(slot >> s.page_log2) * s.page_bytes() + (int64_t)head * s.block_bytes();
@@ -149,9 +176,9 @@ __global__ __launch_bounds__(WAVES * 64) void paged_append_kernel(PagedShape s, 
             if ((j & 7) == 0) *reinterpret_cast<uint32_t*>(block + s.page * D + (t * NG + (j >> 3)) * 4) = p.pair;
             continue;
         }
-        // values: the quad that starts here, whose last rows may be the next wave's, then rows that are in none
+        // values: the quad that starts here, then rows that are in none
         if (lead >= 0) {
-            const Packed p = pack(load(lead + sub, exists));
+            const Packed p = pack(here);
             const uint32_t word = turn_over(p.codes);
             const int t = (lead_slot & (s.page - 1)) + sub;
             uint8_t* block = pages + (int64_t)(lead_slot >> s.page_log2) * s.page_bytes() + (int64_t)head * s.block_bytes();
@@ -161,7 +188,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_append_kernel(PagedShape s, 
             }
         }
         if (__any(alone)) {
-            const Packed p = pack(load(row, alone && exists));
+            const Packed p = pack(lead >= 0 ? load(part, row, alone) : here);
             if (alone && exists) {
                 const int t = slot & (s.page - 1);
                 uint8_t* block = pages + (int64_t)(slot >> s.page_log2) * s.page_bytes() + (int64_t)head * s.block_bytes();
@@ -172,14 +199,15 @@ __global__ __launch_bounds__(WAVES * 64) void paged_append_kernel(PagedShape s, 
             }
         }
     }
+    }
 }
 
 // A lane has 8 columns of a head; of values it reads the four words that hold its bytes beside those of the neighbouring positions, which as
 // a rule other rows of the wave need.
-template <int D>
+template <int D, int U>                 // heads that a lane has
 __global__ __launch_bounds__(WAVES * 64) void paged_read_kernel(PagedShape s, const uint8_t* __restrict__ pages, const int32_t* __restrict__ slots,
                                                                 int rows, _Float16* __restrict__ kv, int64_t ld) {
-    constexpr int LANES = D / 8, SIDE = 16 / LANES, NG = D / 64, U = 2;
+    constexpr int LANES = D / 8, SIDE = 16 / LANES, NG = D / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane >> 4, j = lane & (LANES - 1);
     const int row = blockIdx.x * 4 + sub;
     const int slot = row < rows ? slots[row] : -1;
@@ -215,7 +243,7 @@ __global__ __launch_bounds__(WAVES * 64) void paged_read_kernel(PagedShape s, co
         half8 out;
 #pragma unroll
         for (int i = 0; i < 8; ++i) out[i] = (_Float16)((float)(codes[u] >> (4 * i) & 15u) * (float)pair.h[0] + (float)pair.h[1]);
-        *to[u] = out;
+        __builtin_nontemporal_store(out, to[u]);
     }
 }
 
@@ -228,7 +256,7 @@ int launch_paged_append(const PagedShape& s, const void* qkv, int64_t ld, const 
     // Eight heads a wave, whose slots and angles are then looked up once; one where that would leave the GPU's 1024 SIMDs without two waves each
     const bool many = quads * units >= 8 * 2048;
     auto launch = [&](auto kern, int heads) -> int {
-        const dim3 grid((unsigned)quads, (unsigned)((units + WAVES * heads - 1) / (WAVES * heads)));
+        const dim3 grid((unsigned)((quads + WAVES - 1) / WAVES), (unsigned)((units + heads - 1) / heads));
         hipLaunchKernelGGL(kern, grid, dim3(WAVES * 64), 0, st, s, (const _Float16*)qkv, ld, slots, positions, rows, (const float2*)rope, n_pos,
                            (_Float16*)q_out, ldq, (uint8_t*)pages);
         KVPR_HIP(hipGetLastError());
@@ -240,8 +268,10 @@ int launch_paged_append(const PagedShape& s, const void* qkv, int64_t ld, const 
 
 int launch_paged_read(const PagedShape& s, const void* pages, const int32_t* slots, int rows, void* kv, int64_t ld, hipStream_t st) {
     const int units = (2 * s.kv_heads * s.d + 127) / 128;
-    const dim3 grid((unsigned)(((int64_t)rows + 3) / 4), (unsigned)((units + 2 * WAVES - 1) / (2 * WAVES)));
-    auto kern = s.d == 128 ? paged_read_kernel<128> : paged_read_kernel<64>;
+    const int64_t quads = ((int64_t)rows + 3) / 4;
+    const int each = quads * units >= 8 * 2048 ? 4 : 1;      // as above
+    const dim3 grid((unsigned)quads, (unsigned)((units + each * WAVES - 1) / (each * WAVES)));
+    auto kern = s.d == 128 ? (each == 4 ? paged_read_kernel<128, 4> : paged_read_kernel<128, 1>) : each == 4 ? paged_read_kernel<64, 4> : paged_read_kernel<64, 1>;
     hipLaunchKernelGGL(kern, grid, dim3(WAVES * 64), 0, st, s, (const uint8_t*)pages, slots, rows, (_Float16*)kv, ld);
     KVPR_HIP(hipGetLastError());
     return KVPR_OK;
