@@ -17,11 +17,15 @@
 //     times that of its own rounding), summed in float32.  ref is the largest score less 6 when it was
 //     last set and is set again only when a weight would pass 2^15: no reduction over lanes in the usual turn, and
 //     weights keep all bits down to 2^-20 of the largest, some to 2^-30.
-// Work is split over key/value heads, requests, tiles of rows and chunks of positions; inside a workgroup the waves take turns of 32
-// positions (few rows) or rows of their own (many rows).  Partial sums of a request of several chunks meet in the workspace.
+// Work: a unit is (request, key/value head, tile of rows); few rows: the workgroup's waves share a tile and take turns of 32 positions,
+// many rows: each wave has rows of its own.  The lengths are known on the device only, so every workgroup adds up the requests' turns by
+// itself and takes an equal run of all turns, whatever units that covers; what belongs to a unit of several workgroups meets in the
+// workspace and is joined by a second launch.  (One workgroup per unit and chunk of 2048 positions: 64 requests of
+// 1 to 8192 positions 80 us, most of it starts of workgroups with little or nothing to do.)
 #include "paged.h"
 #include <math.h>
 #include <algorithm>
+#include <type_traits>
 
 namespace kvpr {
 namespace {
@@ -60,25 +64,91 @@ union Half8 {
     half2v h[4];
 };
 
+constexpr int NW = 4;                   // waves of a workgroup
+
 struct AttentionArgs {
     PagedShape s;
     const void* q;
     const uint8_t* pages;
     const int32_t *table, *row_start, *seq_len;
     _Float16* z;
-    float *acc, *ml;                    // partial sums [split][row * heads + head][d], (reference, sum of weights) likewise
+    float* part;                        // partial sums [workgroup][2][slot_rows][d + 2]: the sums, then (reference, sum of weights)
     int64_t ldq, ldz;
-    int rows, group, chunk, row_tiles;
+    int n, rows, group, slot_rows;
     float scale_log2;
 };
+constexpr int FEW = 64;                 // rows up to which a workgroup's waves share them
+constexpr int START = 3;                // what a unit costs beside its turns, in turns: lengths, queries, first operands, the join of the waves
 
 // Lengths and page numbers are read through the constant address space, that is by scalar loads: as vector loads each of them waited
 // for all operands on their way.  Nothing writes them while the kernel runs.
 typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 __device__ __forceinline__ ScalarInts scalar(const int32_t* p) { return (ScalarInts)(uintptr_t)p; }
 
-// what the chunks of a request are, for the kernels on both sides of the workspace
-__device__ __forceinline__ int span_of(const AttentionArgs& a, int r) { return min(max(scalar(a.seq_len)[r], 0), a.s.width * a.s.page); }
+// one request's work, for the kernels on both sides of the workspace
+struct Request {
+    int first, m, len, span;
+    int real;                           // rows per key/value head that there are
+    bool own_rows;                      // each wave has rows of its own
+    int tile_rows, step;                // rows of a unit, positions of a turn
+    int tiles;
+    int turns;                          // of a unit
+    int cost;                           // of a unit, in turns: START for its beginning and end, then its turns
+    int64_t units, work;
+};
+template <int MT, bool OWN>
+__device__ __forceinline__ Request request(const AttentionArgs& a, int r) {
+    Request q;
+    q.first = scalar(a.row_start)[r];
+    q.m = scalar(a.row_start)[r + 1] - q.first;
+    q.len = scalar(a.seq_len)[r];
+    q.span = min(max(q.len, 0), a.s.width * a.s.page);
+    const int there = q.first < 0 ? 0 : max(min(q.m, a.rows - q.first), 0);
+    q.real = there * a.group;
+    q.own_rows = OWN && q.real > FEW;
+    q.tile_rows = MT * 16 * (q.own_rows ? NW : 1);
+    q.step = q.own_rows ? TURN : NW * TURN;
+    q.tiles = (int)((unsigned)(q.real + q.tile_rows - 1) / (unsigned)q.tile_rows);
+    q.turns = max((q.span + q.step - 1) / q.step, 1);
+    q.units = (int64_t)q.tiles * a.s.kv_heads;
+    q.cost = q.turns + START;
+    q.work = q.units * q.cost;
+    return q;
+}
+
+// exclusive sum of v over the 256 threads of the workgroup
+__device__ __forceinline__ int64_t sum_before(int64_t v, int64_t* lds, int64_t& total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t s = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t u = __shfl_up(s, o);
+        if (lane >= o) s += u;
+    }
+    if (lane == 63) lds[wave] = s;
+    __syncthreads();
+    int64_t before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        before += w < wave ? lds[w] : 0;
+        total += lds[w];
+    }
+    return before + s - v;
+}
+
+// request().work from vector loads
+template <int MT, bool OWN>
+__device__ __forceinline__ int64_t work_of(const AttentionArgs& a, int r) {
+    const int first = a.row_start[r], m = a.row_start[r + 1] - first, span = min(max(a.seq_len[r], 0), a.s.width * a.s.page);
+    const int real = (first < 0 ? 0 : max(min(m, a.rows - first), 0)) * a.group;
+    const bool own_rows = OWN && real > FEW;
+    const int tile_rows = MT * 16 * (own_rows ? NW : 1), step = own_rows ? TURN : NW * TURN;
+    return (int64_t)((unsigned)(real + tile_rows - 1) / (unsigned)tile_rows) * a.s.kv_heads * (max((span + step - 1) / step, 1) + START);
+}
+
+// workgroup b of `groups` has the turns [total b / groups, total (b + 1) / groups): the one that has turn x
+__device__ __forceinline__ int64_t group_of(int64_t x, int64_t groups, int64_t total) { return ((x + 1) * groups - 1) / total; }
 
 // One turn's operands as they are loaded: the codes, and of the (scale, minimum) pairs of the 32 positions' keys and values, 512
 // bytes, one lane's share.  The pairs go through LDS, where every lane reads those of its four positions: sixteen lanes
@@ -102,37 +172,91 @@ struct Pairs {
     __device__ void clear(int pos, int gr) { w[(pos * NG + gr) >> 2][(pos * NG + gr) & 3] = 0u; }
 };
 
-template <int D, int MT, bool F32, int NW, bool ROWS>
+template <int D, int MT, bool F32, bool OWN, bool DIRECT>
 __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kernel(const AttentionArgs a) {
     constexpr int NG = D / 64, W = D / 32, NT = 2 * W;   // groups, words of codes a lane has per 16 positions, tiles of 16 columns
+    __shared__ float part[NW][4][NT][64];
+    __shared__ half8 q_lds[OWN ? NW : 1][F32 ? MT : 1][W][64];          // of float32 q, what float16 leaves
+    __shared__ uint32_t pair_lds[NW][64 * NG];
+    __shared__ float2 ml[NW][16];
+    __shared__ int64_t sums[NW], found[2];
     const PagedShape& s = a.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m16 = lane & 15, g = lane >> 4;
-    const int kv_head = blockIdx.x % s.kv_heads, tile0 = blockIdx.x / s.kv_heads, r = blockIdx.y;
-    const int first = scalar(a.row_start)[r], m = scalar(a.row_start)[r + 1] - first, len = scalar(a.seq_len)[r], span = span_of(a, r);
-    const int chunks = max((span + a.chunk - 1) / a.chunk, 1);
-    const int c0 = blockIdx.z * a.chunk, c1 = blockIdx.z == gridDim.z - 1 ? span : min(span, c0 + a.chunk);
-    if (c0 > 0 && c0 >= span) return;                                   // chunk 0 is there for empty requests too
-    const int all_rows = (first < 0 ? 0 : max(min(m, a.rows - first), 0)) * a.group;     // at most 2^30
-    const ScalarInts ids = scalar(a.table) + (int64_t)r * s.width;
-    const int64_t page_bytes = s.page_bytes();
-    const uint8_t* head_base = a.pages + (int64_t)kv_head * s.block_bytes();
-    constexpr int TILE_ROWS = MT * 16 * (ROWS ? NW : 1);
-    __shared__ uint32_t pair_lds[NW][64 * NG];
-    __shared__ float part[ROWS ? 1 : NW][4][NT][64];
-    __shared__ float2 ml[NW][16];
-    __shared__ half8 q_lds[ROWS ? NW : 1][F32 ? MT : 1][W][64];         // of float32 q, what float16 leaves
 
-    for (int row0 = tile0 * TILE_ROWS; row0 < all_rows; row0 += a.row_tiles * TILE_ROWS) {
-        const int wave_row0 = row0 + (ROWS ? wave * MT * 16 : 0), live = min(all_rows - wave_row0, MT * 16);
+    // ---- this workgroup's run of work ----
+    int64_t total = 0, at = 0, end_of_run = 0, offset = 0, b = 0;       // offset: of `at` within the work of request r
+    int r = blockIdx.y;
+    if constexpr (!DIRECT) {
+        const int64_t groups_max = gridDim.x;
+        // consecutive runs to the same XCD (workgroups go round the 8 of them), so that the row tiles of a head meet in one L2
+        b = groups_max % 8 ? blockIdx.x : (blockIdx.x & 7) * (groups_max / 8) + (blockIdx.x >> 3);
+        const int each = (a.n + NW * 64 - 1) / (NW * 64), r0 = min((int)threadIdx.x * each, a.n), r1 = min(r0 + each, a.n);
+        int64_t mine = 0;
+        for (int i = r0; i < r1; ++i) mine += work_of<MT, OWN>(a, i);
+        int64_t before = sum_before(mine, sums, total);
+        const int64_t groups = min(groups_max, total);
+        if (b >= groups) return;
+        at = total * b / groups;
+        end_of_run = total * (b + 1) / groups;
+        if (at >= before && at < before + mine) {
+            for (int i = r0;; ++i) {
+                const int64_t w = work_of<MT, OWN>(a, i);
+                if (at < before + w) {
+                    found[0] = i;
+                    found[1] = at - before;
+                    break;
+                }
+                before += w;
+            }
+        }
+        __syncthreads();
+        r = __builtin_amdgcn_readfirstlane((int)found[0]);
+        offset = (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)found[1]) | (int64_t)__builtin_amdgcn_readfirstlane((int)(found[1] >> 32)) << 32;
+    }
+    const int64_t page_bytes = s.page_bytes();
+
+    Request rq = request<MT, OWN>(a, r);
+    if constexpr (DIRECT) {
+        offset = blockIdx.x;                                // counts units here
+        end_of_run = rq.units;
+    }
+    while (DIRECT ? offset < end_of_run : at < end_of_run) {
+        int64_t unit = offset;
+        int turn0 = 0, turn1 = rq.turns;
+        if constexpr (DIRECT) {
+            offset += gridDim.x;
+        } else {
+            if (offset >= rq.work) {
+                offset -= rq.work;
+                rq = request<MT, OWN>(a, ++r);
+                continue;
+            }
+            unit = offset / rq.cost;
+            const int from = (int)(offset - unit * rq.cost), to = (int)min((int64_t)rq.cost, from + (end_of_run - at));
+            at += to - from;
+            offset += to - from;
+            turn0 = max(from - START, 0);
+            turn1 = to - START;
+            if (turn1 <= turn0) continue;                   // the beginning of a unit whose turns are the next workgroup's
+        }
+        const int kv_head = (int)(unit / rq.tiles);
+        const int row0 = (int)(unit - (int64_t)kv_head * rq.tiles) * rq.tile_rows;
+        const bool own_rows = OWN && rq.own_rows;
+        const int c0 = turn0 * rq.step, c1 = min(rq.span, turn1 * rq.step);
+        const ScalarInts ids = scalar(a.table) + (int64_t)r * s.width;
+        const uint8_t* head_base = a.pages + (int64_t)kv_head * s.block_bytes();
+        const int region = own_rows ? wave : 0, wave_row0 = row0 + region * (MT * 16), live_rows = min(rq.real - wave_row0, MT * 16);
         // positions that every / any row of the wave sees: those of its first and its last row
-        const int see0 = len - m + 1, all_see = min(span, see0 + wave_row0 / a.group),
-                  any_see = live > 0 ? min(span, see0 + (wave_row0 + live - 1) / a.group) : 0;
-        const int end = min(c1, any_see);
+        const int see0 = rq.len - rq.m + 1, all_see = min(rq.span, see0 + wave_row0 / a.group),
+                  any_see = live_rows > 0 ? min(rq.span, see0 + (wave_row0 + live_rows - 1) / a.group) : 0;
+        const int end = min(c1, any_see), step = rq.step;
+        int t0 = c0 + (own_rows ? 0 : wave * TURN);
+
         const int k_lane = m16 * (D / 2) + g * (D / 8), v_lane = s.page * (D / 2) + g * (2 * D) + m16 * (D / 8),
                   p_lane = s.page * D + (NG == 2 ? (lane & 32 ? s.page * 8 : 0) + (lane & 31) * 4 : (lane & 16 ? s.page * 4 : 0) + m16 * 4);
         auto id_of = [&](int t) { return ids[min(t, end - 1) >> s.page_log2]; };     // those behind the end are not used
-        auto load = [&](Turn<D>& x, int t0, const int (&id)[2]) {
+        auto load = [&](Turn<D>& x, int t0, const int (&id)[2]) __attribute__((always_inline)) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 // a half of a turn that lies outside the pool reads its first page and is masked; one behind the end reads what is there
@@ -153,8 +277,6 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
                 x.pairs[u] = __builtin_amdgcn_raw_buffer_load_b32(block, p_lane, tp * (NG * 4), 0);
             }
         };
-        const int step = ROWS ? TURN : NW * TURN;
-        int t0 = c0 + (ROWS ? 0 : wave * TURN);
         // two turns' operands in registers: one at work, one on its way; page numbers one turn further ahead
         Turn<D> xa, xb;
         int ia[2], ib[2];
@@ -166,10 +288,10 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
         // ---- rows: where they are, how far they see, q ----
         // row, head and whether there is one; worked out again at the end rather than kept
         auto place = [&](int mt, int& token, int& head) {
-            const int rr = wave_row0 + mt * 16 + m16, there = min(rr, all_rows - 1), i = there / a.group;
-            token = first + i;
+            const int rr = wave_row0 + mt * 16 + m16, there = min(rr, rq.real - 1), i = there / a.group;
+            token = rq.first + i;
             head = kv_head * a.group + there - i * a.group;
-            return rr < all_rows;
+            return rr < rq.real;
         };
         int seen[MT];
         bool real[MT];
@@ -179,7 +301,7 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
         for (int mt = 0; mt < MT; ++mt) {
             int token, head;
             real[mt] = place(mt, token, head);
-            seen[mt] = real[mt] ? min(span, len - m + (token - first) + 1) : 0;
+            seen[mt] = real[mt] ? min(rq.span, see0 + token - rq.first) : 0;
             const int64_t at = real[mt] ? token * a.ldq + (int64_t)head * D : 0;
             float x[W][8], big = 0.f;
 #pragma unroll
@@ -224,7 +346,7 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
                     if constexpr (F32) rest.v[e] = (_Float16)(y - (float)hi);
                 }
                 // the waves that share rows write the same
-                if constexpr (F32) q_lds[ROWS ? wave : 0][mt][st][lane] = rest.v;
+                if constexpr (F32) q_lds[region][mt][st][lane] = rest.v;
             }
         }
 
@@ -241,7 +363,7 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
         // in a register, so that masking and setting the upper bits are one instruction (with two literals they are two)
         uint32_t magic = 0x64006400u;
         asm("" : "+v"(magic));
-        auto compute = [&](const Turn<D>& x, int t0, const int (&id)[2]) {
+        auto compute = [&](const Turn<D>& x, int t0, const int (&id)[2]) __attribute__((always_inline)) {
             const bool masked = t0 + TURN > min(all_see, c1) || (unsigned)id[0] >= (unsigned)s.n_pages || (unsigned)id[1] >= (unsigned)s.n_pages;
             uint32_t* mine = pair_lds[wave];
 #pragma unroll
@@ -279,7 +401,7 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
 #pragma unroll
                 for (int st = 0; st < W; ++st) {
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) ql[mt] = q_lds[ROWS ? wave : 0][mt][st][lane];
+                    for (int mt = 0; mt < MT; ++mt) ql[mt] = q_lds[region][mt][st][lane];
                     score(0, st, ql);
                     score(1, st, ql);
                 }
@@ -424,29 +546,32 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
         for (int mt = 0; mt < MT; ++mt) {
             l[mt] = across_rows(l[mt], sum_of);
         }
+        const bool all_here = DIRECT || (turn0 == 0 && turn1 == rq.turns);
+        float* slot = a.part + ((b * 2 + (turn0 == 0)) * a.slot_rows + region * (MT * 16)) * (D + 2);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            if (row0 + mt * 16 >= all_rows) break;
+            if (mt * 16 >= live_rows) break;
             int token, head;
-            const bool there = place(mt, token, head);
-            float top = ref[mt], sum = l[mt];
+            const bool real = place(mt, token, head);
+            float lsum = l[mt], top = ref[mt];
             // columns 64 gr + 16 g + 4 p .. + 3 of one row from acc over (w, h)
             auto put = [&](int p, int gr, const float (&what)[4]) {
-                if (!there) return;
+                if (!real) return;
                 const int col = 64 * gr + (4 * g + p) * 4;
-                if (chunks == 1 || gridDim.z == 1) {
-                    const float inv = 1.f / sum;
+                if (all_here) {
+                    const float inv = 1.f / lsum;
                     half4 out;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) out[e] = (_Float16)(sum == 0.f ? 0.f : what[e] * inv);
+                    for (int e = 0; e < 4; ++e) out[e] = (_Float16)(lsum == 0.f ? 0.f : what[e] * inv);
                     *reinterpret_cast<half4*>(a.z + token * a.ldz + (int64_t)head * D + col) = out;
                 } else {
-                    const int64_t slot = ((int64_t)blockIdx.z * a.rows + token) * s.heads + head;
-                    *reinterpret_cast<float4v*>(a.acc + slot * D + col) = float4v{what[0], what[1], what[2], what[3]};
-                    if (col == 0) *reinterpret_cast<float2*>(a.ml + slot * 2) = make_float2(top, sum);
+                    float* to = slot + (mt * 16 + m16) * (D + 2);
+                    *reinterpret_cast<float2*>(to + col) = make_float2(what[0], what[1]);
+                    *reinterpret_cast<float2*>(to + col + 2) = make_float2(what[2], what[3]);
+                    if (col == 0) *reinterpret_cast<float2*>(to + D) = make_float2(top, lsum);
                 }
             };
-            if constexpr (ROWS) {
+            if (own_rows) {
 #pragma unroll
                 for (int p = 0; p < 4; ++p)
 #pragma unroll
@@ -456,15 +581,15 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
                     }
             } else {
                 // the waves' sums meet in LDS, a tile of rows at a time; wave w then has the columns of p = w
-                if (mt || row0 != tile0 * TILE_ROWS) __syncthreads();
-                if (g == 0) ml[wave][m16] = make_float2(top, sum);
+                if (mt) __syncthreads();
+                if (g == 0) ml[wave][m16] = make_float2(top, lsum);
                 __syncthreads();
                 float all_top = LOWEST;
-                sum = 0.f;
+                lsum = 0.f;
 #pragma unroll
                 for (int w = 0; w < NW; ++w) all_top = fmaxf(all_top, ml[w][m16].x);
 #pragma unroll
-                for (int w = 0; w < NW; ++w) sum += ml[w][m16].y * exp2f(ml[w][m16].x - all_top);
+                for (int w = 0; w < NW; ++w) lsum += ml[w][m16].y * exp2f(ml[w][m16].x - all_top);
                 const float mine = exp2f(top - all_top);
                 top = all_top;
 #pragma unroll
@@ -483,111 +608,137 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
                 }
             }
         }
+        __syncthreads();
     }
 }
 
-// Joins the chunks of requests that have several: one wave per (row, head).
-template <int D>
-__global__ __launch_bounds__(256) void paged_attention_join(const AttentionArgs a) {
-    constexpr int E = D / 64;
+// Joins the units of several workgroups: one wave per (row, head).
+template <int D, int MT, bool OWN>
+__global__ __launch_bounds__(NW * 64) void paged_attention_join(const AttentionArgs a, int64_t groups_max) {
+    constexpr int E = D / 64, U = 8;
+    __shared__ int64_t sums[NW];
     const int lane = threadIdx.x & 63, r = blockIdx.y;
-    const int span = span_of(a, r), chunks = min((span + a.chunk - 1) / a.chunk, a.row_tiles);   // row_tiles: chunks of the launch
-    if (chunks <= 1) return;
-    const int first = a.row_start[r];
-    const int64_t pairs = (int64_t)(a.row_start[r + 1] - first) * a.s.heads;
-    for (int64_t j = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); j < pairs; j += (int64_t)gridDim.x * 4) {
-        const int64_t token = first + j / a.s.heads, head = j % a.s.heads;
-        if (token < 0 || token >= a.rows) return;
-        const int64_t at = token * a.s.heads + head, stride = (int64_t)a.rows * a.s.heads;
-        float top = LOWEST, l = 0.f, o[E] = {};
-        for (int c = 0; c < chunks; ++c) top = fmaxf(top, a.ml[(c * stride + at) * 2]);
-        for (int c = 0; c < chunks; ++c) {
-            const float2 ml = *reinterpret_cast<const float2*>(a.ml + (c * stride + at) * 2);
-            const float w = exp2f(ml.x - top);
-            l += ml.y * w;
-            const float* p = a.acc + (c * stride + at) * D + lane * E;
+    const Request rq = request<MT, OWN>(a, r);
+    int64_t before = 0, total = 0;
+    for (int i = threadIdx.x; i < a.n; i += NW * 64) {
+        const int64_t w = work_of<MT, OWN>(a, i);
+        before += i < r ? w : 0;
+        total += w;
+    }
+    int64_t sum;
+    sum_before(before, sums, sum);
+    before = sum;
+    __syncthreads();
+    sum_before(total, sums, sum);
+    total = sum;
+    const int64_t groups = min(groups_max, total), pairs = (int64_t)rq.real * a.s.kv_heads;
+    for (int64_t j = (int64_t)blockIdx.x * NW + (threadIdx.x >> 6); j < pairs; j += (int64_t)gridDim.x * NW) {
+        const int kv_head = (int)(j / rq.real);
+        const int rr = (int)(j - (int64_t)kv_head * rq.real), tile = rr / rq.tile_rows;
+        const int64_t x0 = before + ((int64_t)kv_head * rq.tiles + tile) * rq.cost + START;
+        const int64_t b0 = group_of(x0, groups, total), b1 = group_of(x0 + rq.turns - 1, groups, total);
+        if (b0 == b1) continue;
+        const int64_t stride = 2 * (int64_t)a.slot_rows * (D + 2);
+        const float* from = a.part + b0 * stride + (rr - tile * rq.tile_rows) * (D + 2);     // slot 1 of b0, slot 0 of those behind it
+        const int pieces = (int)(b1 - b0) + 1;
+        auto piece = [&](int c) { return from + c * stride + (c == 0 ? (int64_t)a.slot_rows * (D + 2) : 0); };
+        float top = LOWEST;
+        for (int c = lane; c < pieces; c += 64) top = fmaxf(top, piece(c)[D]);
+        for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+        float l = 0.f, o[E] = {};
+        for (int c0 = 0; c0 < pieces; c0 += U) {
+            float2 ml[U];
+            float x[U][E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] += p[e] * w;
+            for (int u = 0; u < U; ++u) {
+                const float* p = piece(min(c0 + u, pieces - 1));
+                ml[u] = *reinterpret_cast<const float2*>(p + D);
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[u][e] = p[lane * E + e];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (c0 + u >= pieces) continue;
+                const float w = exp2f(ml[u].x - top);
+                l += ml[u].y * w;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] += x[u][e] * w;
+            }
         }
+        const int64_t token = rq.first + rr / a.group, head = kv_head * a.group + rr % a.group;
         _Float16* z = a.z + token * a.ldz + head * D + lane * E;
 #pragma unroll
         for (int e = 0; e < E; ++e) z[e] = (_Float16)(l == 0.f ? 0.f : o[e] / l);
     }
 }
 
-// how a launch is cut
+// how a launch is cut, from what the host knows
 struct Cut {
-    int mt;             // tiles of 16 rows a wave
-    bool rows;          // the waves of a workgroup have rows of their own
-    int row_tiles, chunk, chunks;
+    int mt;                             // tiles of 16 rows a wave
+    bool many_rows, direct;
+    int groups, slot_rows;
 };
-constexpr int NW = 4;
 
-Cut cut_of(const PagedShape& s, int n, int max_new, int max_len, bool) {
+Cut cut_of(const PagedShape& s, int n, int rows, int max_new, int max_len) {
     Cut c;
-    const int64_t r = (int64_t)max_new * (s.heads / s.kv_heads);
+    const int64_t r = (int64_t)std::min(max_new, std::max(rows, 1)) * (s.heads / s.kv_heads);
     c.mt = r <= 16 ? 1 : 2;
-    c.rows = r > 128;
-    const int tile = c.mt * 16 * (c.rows ? NW : 1);
-    c.row_tiles = (int)std::min<int64_t>((r + tile - 1) / tile, 65535 / 8);
-    const int64_t len = std::min<int64_t>(max_len, (int64_t)s.width * s.page);
-    const int64_t units = (int64_t)n * s.kv_heads * c.row_tiles;
-    const int64_t want = std::max<int64_t>(1, (c.rows ? 512 : 1024) / units), least = c.rows ? 512 : NW * TURN;
-    int64_t chunk = std::max(least, (len + want - 1) / want);
-    if (!c.rows) chunk = std::min<int64_t>(chunk, 2048);
-    chunk = (chunk + NW * TURN - 1) / (NW * TURN) * (NW * TURN);
-    chunk = std::max(chunk, (len + 1023) / 1024 / (NW * TURN) * (NW * TURN));     // at most about 1024 chunks
-    c.chunk = (int)std::min<int64_t>(chunk, 0x7fffffff / 2);
-    c.chunks = (int)std::max<int64_t>(1, (len + c.chunk - 1) / c.chunk);
+    c.many_rows = r > FEW;
+    c.slot_rows = c.mt * 16 * (c.many_rows ? NW : 1);
+    const int resident = 256 * (c.mt == 1 ? 3 : 2);                        // workgroups that the GPU holds at once
+    const int64_t units = s.kv_heads * ((r + c.slot_rows - 1) / c.slot_rows), all = units * std::min<int64_t>(n, std::max(rows, 1));
+    const int64_t len = std::min<int64_t>(max_len, (int64_t)s.width * s.page), step = c.many_rows ? TURN : NW * TURN;
+    c.direct = len <= step || (c.many_rows ? all >= resident / 2 : all >= resident / 2 && len <= 2048);
+    if (c.direct) {
+        c.groups = (int)std::min<int64_t>(units, 1 << 16);
+    } else {
+        c.groups = (int)std::min<int64_t>(resident, all * ((len + step - 1) / step));
+        if (c.groups > 8) c.groups = (c.groups + 7) / 8 * 8;
+    }
     return c;
 }
-
-int64_t part_floats(const PagedShape& s, int rows, const Cut& c) { return c.chunks > 1 ? (int64_t)c.chunks * rows * s.heads : 0; }
 
 }  // namespace
 
 size_t paged_attention_workspace_bytes(const PagedShape& s, int n, int rows, int max_new, int max_len) {
-    return (size_t)part_floats(s, rows, cut_of(s, n, max_new, max_len, false)) * (s.d + 2) * 4 + 16;
+    const Cut c = cut_of(s, n, rows, max_new, max_len);
+    return c.direct ? 16 : (size_t)c.groups * 2 * c.slot_rows * (s.d + 2) * 4;
 }
 
 int launch_paged_attention(const PagedShape& s, const PagedAttention& x, void* ws, size_t, hipStream_t st) {
-    const Cut c = cut_of(s, x.n, x.max_new, x.max_len, x.q_f32);
+    const Cut c = cut_of(s, x.n, x.rows, x.max_new, x.max_len);
     AttentionArgs a;
     a.s = s;
     a.q = x.q;
     a.pages = (const uint8_t*)x.pages;
     a.table = x.table; a.row_start = x.row_start; a.seq_len = x.seq_len;
     a.z = (_Float16*)x.z;
-    a.acc = (float*)ws;
-    a.ml = a.acc + part_floats(s, x.rows, c) * s.d;
+    a.part = (float*)ws;
     a.ldq = x.ldq; a.ldz = x.ldz;
-    a.rows = x.rows; a.group = s.heads / s.kv_heads; a.chunk = c.chunk; a.row_tiles = c.row_tiles;
+    a.n = x.n; a.rows = x.rows; a.group = s.heads / s.kv_heads; a.slot_rows = c.slot_rows;
     a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)s.d));
-    const dim3 grid((unsigned)(s.kv_heads * c.row_tiles), (unsigned)x.n, (unsigned)c.chunks);
-#define KVPR_LAUNCH(D_, MT_, F32_, ROWS_) hipLaunchKernelGGL((paged_attention_kernel<D_, MT_, F32_, NW, ROWS_>), grid, dim3(NW * 64), 0, st, a)
-#define KVPR_BY_MT(D_, F32_)                                                      \
-    do {                                                                          \
-        if (c.rows) KVPR_LAUNCH(D_, 2, F32_, true);                               \
-        else if (c.mt == 1) KVPR_LAUNCH(D_, 1, F32_, false);                      \
-        else KVPR_LAUNCH(D_, 2, F32_, false);                                     \
-    } while (0)
-    if (s.d == 128) {
-        if (x.q_f32) KVPR_BY_MT(128, true); else KVPR_BY_MT(128, false);
-    } else {
-        if (x.q_f32) KVPR_BY_MT(64, true); else KVPR_BY_MT(64, false);
-    }
-#undef KVPR_BY_MT
-#undef KVPR_LAUNCH
-    KVPR_HIP(hipGetLastError());
-    if (c.chunks > 1) {
-        a.row_tiles = c.chunks;
-        const int64_t pairs = (int64_t)x.max_new * s.heads;
-        const dim3 joined((unsigned)std::min<int64_t>((pairs + 3) / 4, 4096), (unsigned)x.n);
-        if (s.d == 128) hipLaunchKernelGGL(paged_attention_join<128>, joined, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL(paged_attention_join<64>, joined, dim3(256), 0, st, a);
+    const int64_t pairs = (int64_t)std::min(x.max_new, x.rows) * s.heads;
+    const dim3 grid((unsigned)c.groups, c.direct ? (unsigned)x.n : 1), joined((unsigned)std::min<int64_t>((pairs + NW - 1) / NW, std::max(2048 / x.n, 1)), (unsigned)x.n);
+    auto launch = [&](auto kern, auto join) -> int {
+        hipLaunchKernelGGL(kern, grid, dim3(NW * 64), 0, st, a);
         KVPR_HIP(hipGetLastError());
-    }
-    return KVPR_OK;
+        if (c.direct) return KVPR_OK;
+        hipLaunchKernelGGL(join, joined, dim3(NW * 64), 0, st, a, (int64_t)c.groups);
+        KVPR_HIP(hipGetLastError());
+        return KVPR_OK;
+    };
+#define KVPR_CASE(D_, F32_, MT_, OWN_) \
+    if (s.d == D_ && x.q_f32 == F32_ && c.mt == MT_ && c.many_rows == OWN_)                                                                        \
+        return launch(c.direct ? paged_attention_kernel<D_, MT_, F32_, OWN_, true> : paged_attention_kernel<D_, MT_, F32_, OWN_, false>, paged_attention_join<D_, MT_, OWN_>)
+#define KVPR_CASES(D_, F32_)                                                                    \
+    KVPR_CASE(D_, F32_, 1, false); KVPR_CASE(D_, F32_, 2, false); KVPR_CASE(D_, F32_, 2, true)
+    KVPR_CASES(64, false);
+    KVPR_CASES(64, true);
+    KVPR_CASES(128, false);
+    KVPR_CASES(128, true);
+#undef KVPR_CASES
+#undef KVPR_CASE
+    return fail(KVPR_E_STATE, "no kernel for %d tiles", c.mt);
 }
 
 }  // namespace kvpr
