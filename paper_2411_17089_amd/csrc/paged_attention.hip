@@ -17,15 +17,17 @@
 //     times that of its own rounding), summed in float32.  ref is the largest score less 6 when it was
 //     last set and is set again only when a weight would pass 2^15: no reduction over lanes in the usual turn, and
 //     weights keep all bits down to 2^-20 of the largest, some to 2^-30.
-// Work: a unit is (request, key/value head, tile of rows); few rows: the workgroup's waves share a tile and take turns of 32 positions,
-// many rows: each wave has rows of its own.  The lengths are known on the device only, so every workgroup adds up the requests' turns by
-// itself and takes an equal run of all turns, whatever units that covers; what belongs to a unit of several workgroups meets in the
-// workspace and is joined by a second launch.  (One workgroup per unit and chunk of 2048 positions: 64 requests of
-// 1 to 8192 positions 80 us, most of it starts of workgroups with little or nothing to do.)
+// What bounds it: long caches with one row a request the reading (32 x 1000 positions of 32 heads 36 us, 4.1 TB/s of packed rows); more
+// rows a head the vector instructions between the products (unpacking 160 a turn and wave, 100 more for each tile of rows).
+// Work: a unit is (request, key/value head, tile of rows).  Few rows: the workgroup's waves share a tile and take turns of 32 positions in
+// turn, their sums meet in LDS; many rows: each wave has rows of its own.  The lengths are known on the device only.  Where the
+// host's bounds let them differ much, every workgroup adds up the requests' work by itself and takes an equal run of it, whatever units
+// that covers; what belongs to a unit of several workgroups meets in the workspace and is joined by a second launch.  (One workgroup
+// per unit and chunk of 2048 positions: 64 requests of 1 to 8192 positions 79 us, most of it starts of workgroups with little or
+// nothing to do; by runs 52.)  Elsewhere a workgroup has a unit, and there is no second launch.
 #include "paged.h"
 #include <math.h>
 #include <algorithm>
-#include <type_traits>
 
 namespace kvpr {
 namespace {
@@ -73,10 +75,13 @@ struct AttentionArgs {
     const int32_t *table, *row_start, *seq_len;
     _Float16* z;
     float* part;                        // partial sums [workgroup][2][slot_rows][d + 2]: the sums, then (reference, sum of weights)
+    struct Open* open;                  // [workgroup]
     int64_t ldq, ldz;
     int n, rows, group, slot_rows;
     float scale_log2;
 };
+// the unit that a workgroup began and left to those behind it: pieces = 0: none
+struct Open { int pieces, first, row0, real, kv_head; };
 constexpr int FEW = 64;                 // rows up to which a workgroup's waves share them
 constexpr int START = 3;                // what a unit costs beside its turns, in turns: lengths, queries, first operands, the join of the waves
 
@@ -85,7 +90,7 @@ constexpr int START = 3;                // what a unit costs beside its turns, i
 typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 __device__ __forceinline__ ScalarInts scalar(const int32_t* p) { return (ScalarInts)(uintptr_t)p; }
 
-// one request's work, for the kernels on both sides of the workspace
+// one request's work
 struct Request {
     int first, m, len, span;
     int real;                           // rows per key/value head that there are
@@ -185,7 +190,7 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
     const int m16 = lane & 15, g = lane >> 4;
 
     // ---- this workgroup's run of work ----
-    int64_t total = 0, at = 0, end_of_run = 0, offset = 0, b = 0;       // offset: of `at` within the work of request r
+    int64_t total = 0, groups = 0, at = 0, end_of_run = 0, offset = 0, b = 0;       // offset: of `at` within the work of request r
     int r = blockIdx.y;
     if constexpr (!DIRECT) {
         const int64_t groups_max = gridDim.x;
@@ -195,7 +200,8 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
         int64_t mine = 0;
         for (int i = r0; i < r1; ++i) mine += work_of<MT, OWN>(a, i);
         int64_t before = sum_before(mine, sums, total);
-        const int64_t groups = min(groups_max, total);
+        groups = min(groups_max, total);
+        if (threadIdx.x == 0) a.open[b].pieces = 0;
         if (b >= groups) return;
         at = total * b / groups;
         end_of_run = total * (b + 1) / groups;
@@ -543,10 +549,10 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
             }
         }
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            l[mt] = across_rows(l[mt], sum_of);
-        }
+        for (int mt = 0; mt < MT; ++mt) l[mt] = across_rows(l[mt], sum_of);
         const bool all_here = DIRECT || (turn0 == 0 && turn1 == rq.turns);
+        if (!all_here && turn0 == 0 && threadIdx.x == 0)    // the rest of the turns end in the workgroup that has the last of them
+            a.open[b] = Open{(int)(group_of(at + (rq.turns - turn1) - 1, groups, total) - b) + 1, rq.first, row0, rq.real, kv_head};
         float* slot = a.part + ((b * 2 + (turn0 == 0)) * a.slot_rows + region * (MT * 16)) * (D + 2);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
@@ -612,64 +618,49 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
     }
 }
 
-// Joins the units of several workgroups: one wave per (row, head).
-template <int D, int MT, bool OWN>
-__global__ __launch_bounds__(NW * 64) void paged_attention_join(const AttentionArgs a, int64_t groups_max) {
-    constexpr int E = D / 64, U = 8;
-    __shared__ int64_t sums[NW];
-    const int lane = threadIdx.x & 63, r = blockIdx.y;
-    const Request rq = request<MT, OWN>(a, r);
-    int64_t before = 0, total = 0;
-    for (int i = threadIdx.x; i < a.n; i += NW * 64) {
-        const int64_t w = work_of<MT, OWN>(a, i);
-        before += i < r ? w : 0;
-        total += w;
-    }
-    int64_t sum;
-    sum_before(before, sums, sum);
-    before = sum;
-    __syncthreads();
-    sum_before(total, sums, sum);
-    total = sum;
-    const int64_t groups = min(groups_max, total), pairs = (int64_t)rq.real * a.s.kv_heads;
-    for (int64_t j = (int64_t)blockIdx.x * NW + (threadIdx.x >> 6); j < pairs; j += (int64_t)gridDim.x * NW) {
-        const int kv_head = (int)(j / rq.real);
-        const int rr = (int)(j - (int64_t)kv_head * rq.real), tile = rr / rq.tile_rows;
-        const int64_t x0 = before + ((int64_t)kv_head * rq.tiles + tile) * rq.cost + START;
-        const int64_t b0 = group_of(x0, groups, total), b1 = group_of(x0 + rq.turns - 1, groups, total);
-        if (b0 == b1) continue;
-        const int64_t stride = 2 * (int64_t)a.slot_rows * (D + 2);
-        const float* from = a.part + b0 * stride + (rr - tile * rq.tile_rows) * (D + 2);     // slot 1 of b0, slot 0 of those behind it
-        const int pieces = (int)(b1 - b0) + 1;
-        auto piece = [&](int c) { return from + c * stride + (c == 0 ? (int64_t)a.slot_rows * (D + 2) : 0); };
-        float top = LOWEST;
-        for (int c = lane; c < pieces; c += 64) top = fmaxf(top, piece(c)[D]);
-        for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-        float l = 0.f, o[E] = {};
-        for (int c0 = 0; c0 < pieces; c0 += U) {
-            float2 ml[U];
-            float x[U][E];
+// Joins the units of several workgroups: a wave has one row of the unit that workgroup x of the first launch left open, and asks for 16 of
+// its pieces at once, since what counts is the wait for them.
+constexpr int JOIN_ROWS = 16;           // of a workgroup: most have nothing to do, so there are few of them
+template <int D>
+__global__ __launch_bounds__(JOIN_ROWS * 64) void paged_attention_join(const AttentionArgs a) {
+    constexpr int E = D / 64, U = 16;
+    const int lane = threadIdx.x & 63, row = blockIdx.y * JOIN_ROWS + (threadIdx.x >> 6);
+    const Open o = a.open[blockIdx.x];
+    const int rr = o.row0 + row;
+    if (o.pieces == 0 || rr >= o.real) return;
+    const int64_t stride = 2 * (int64_t)a.slot_rows * (D + 2);
+    const float* from = a.part + blockIdx.x * stride + (int64_t)row * (D + 2);          // slot 1 of the first, slot 0 of those behind it
+    float top = LOWEST, l = 0.f, sum[E] = {};
+    for (int c0 = 0; c0 < o.pieces; c0 += U) {
+        float2 ml[U];
+        float x[U][E];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const float* p = piece(min(c0 + u, pieces - 1));
-                ml[u] = *reinterpret_cast<const float2*>(p + D);
-#pragma unroll
-                for (int e = 0; e < E; ++e) x[u][e] = p[lane * E + e];
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (c0 + u >= pieces) continue;
-                const float w = exp2f(ml[u].x - top);
-                l += ml[u].y * w;
-#pragma unroll
-                for (int e = 0; e < E; ++e) o[e] += x[u][e] * w;
-            }
+        for (int u = 0; u < U; ++u) {
+            const int c = min(c0 + u, o.pieces - 1);
+            const float* p = from + c * stride + (c == 0 ? (int64_t)a.slot_rows * (D + 2) : 0);
+            ml[u] = *reinterpret_cast<const float2*>(p + D);
+            __builtin_memcpy(x[u], p + lane * E, 4 * E);
         }
-        const int64_t token = rq.first + rr / a.group, head = kv_head * a.group + rr % a.group;
-        _Float16* z = a.z + token * a.ldz + head * D + lane * E;
+        float now = top;
 #pragma unroll
-        for (int e = 0; e < E; ++e) z[e] = (_Float16)(l == 0.f ? 0.f : o[e] / l);
+        for (int u = 0; u < U; ++u) now = fmaxf(now, ml[u].x);
+        const float keep = exp2f(top - now);
+        top = now;
+        l *= keep;
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] *= keep;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float w = c0 + u < o.pieces ? exp2f(ml[u].x - top) : 0.f;
+            l = fmaf(ml[u].y, w, l);
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] = fmaf(x[u][e], w, sum[e]);
+        }
     }
+    const int64_t token = o.first + rr / a.group, head = o.kv_head * a.group + rr % a.group;
+    _Float16* z = a.z + token * a.ldz + head * D + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) z[e] = (_Float16)(l == 0.f ? 0.f : sum[e] / l);
 }
 
 // how a launch is cut, from what the host knows
@@ -688,6 +679,10 @@ Cut cut_of(const PagedShape& s, int n, int rows, int max_new, int max_len) {
     const int resident = 256 * (c.mt == 1 ? 3 : 2);                        // workgroups that the GPU holds at once
     const int64_t units = s.kv_heads * ((r + c.slot_rows - 1) / c.slot_rows), all = units * std::min<int64_t>(n, std::max(rows, 1));
     const int64_t len = std::min<int64_t>(max_len, (int64_t)s.width * s.page), step = c.many_rows ? TURN : NW * TURN;
+    // A unit each for a workgroup, or equal runs of the work: runs cost a second launch and the sums in front of the first, 9 us in all, and
+    // units that differ in length keep the GPU waiting for the longest.  us by units / by runs: 32 x 1000 positions, 32 heads 36 / 45; 64 x 1 to
+    // 8192, 8 heads 104 / 52; 4 x 25000, 8 heads 276 / 64; two chunks of 1000 rows 215 / 270.  So units where they fill half of the GPU and none
+    // is longer than 16 turns, or where their rows are many, and where a unit has one turn.
     c.direct = len <= step || (c.many_rows ? all >= resident / 2 : all >= resident / 2 && len <= 2048);
     if (c.direct) {
         c.groups = (int)std::min<int64_t>(units, 1 << 16);
@@ -702,7 +697,7 @@ Cut cut_of(const PagedShape& s, int n, int rows, int max_new, int max_len) {
 
 size_t paged_attention_workspace_bytes(const PagedShape& s, int n, int rows, int max_new, int max_len) {
     const Cut c = cut_of(s, n, rows, max_new, max_len);
-    return c.direct ? 16 : (size_t)c.groups * 2 * c.slot_rows * (s.d + 2) * 4;
+    return c.direct ? 16 : (size_t)c.groups * (2 * (size_t)c.slot_rows * (s.d + 2) * 4 + sizeof(Open));
 }
 
 int launch_paged_attention(const PagedShape& s, const PagedAttention& x, void* ws, size_t, hipStream_t st) {
@@ -714,22 +709,23 @@ int launch_paged_attention(const PagedShape& s, const PagedAttention& x, void* w
     a.table = x.table; a.row_start = x.row_start; a.seq_len = x.seq_len;
     a.z = (_Float16*)x.z;
     a.part = (float*)ws;
+    a.open = (Open*)(a.part + (size_t)c.groups * 2 * c.slot_rows * (s.d + 2));
     a.ldq = x.ldq; a.ldz = x.ldz;
     a.n = x.n; a.rows = x.rows; a.group = s.heads / s.kv_heads; a.slot_rows = c.slot_rows;
     a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)s.d));
-    const int64_t pairs = (int64_t)std::min(x.max_new, x.rows) * s.heads;
-    const dim3 grid((unsigned)c.groups, c.direct ? (unsigned)x.n : 1), joined((unsigned)std::min<int64_t>((pairs + NW - 1) / NW, std::max(2048 / x.n, 1)), (unsigned)x.n);
-    auto launch = [&](auto kern, auto join) -> int {
+    const dim3 grid((unsigned)c.groups, c.direct ? (unsigned)x.n : 1), joined((unsigned)c.groups, (unsigned)(c.slot_rows / JOIN_ROWS));
+    auto launch = [&](auto kern) -> int {
         hipLaunchKernelGGL(kern, grid, dim3(NW * 64), 0, st, a);
         KVPR_HIP(hipGetLastError());
         if (c.direct) return KVPR_OK;
-        hipLaunchKernelGGL(join, joined, dim3(NW * 64), 0, st, a, (int64_t)c.groups);
+        if (s.d == 128) hipLaunchKernelGGL(paged_attention_join<128>, joined, dim3(JOIN_ROWS * 64), 0, st, a);
+        else hipLaunchKernelGGL(paged_attention_join<64>, joined, dim3(JOIN_ROWS * 64), 0, st, a);
         KVPR_HIP(hipGetLastError());
         return KVPR_OK;
     };
 #define KVPR_CASE(D_, F32_, MT_, OWN_) \
     if (s.d == D_ && x.q_f32 == F32_ && c.mt == MT_ && c.many_rows == OWN_)                                                                        \
-        return launch(c.direct ? paged_attention_kernel<D_, MT_, F32_, OWN_, true> : paged_attention_kernel<D_, MT_, F32_, OWN_, false>, paged_attention_join<D_, MT_, OWN_>)
+        return launch(c.direct ? paged_attention_kernel<D_, MT_, F32_, OWN_, true> : paged_attention_kernel<D_, MT_, F32_, OWN_, false>)
 #define KVPR_CASES(D_, F32_)                                                                    \
     KVPR_CASE(D_, F32_, 1, false); KVPR_CASE(D_, F32_, 2, false); KVPR_CASE(D_, F32_, 2, true)
     KVPR_CASES(64, false);
