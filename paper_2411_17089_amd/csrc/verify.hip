@@ -381,7 +381,8 @@ __global__ __launch_bounds__(THREADS) void verify_draw(const VerifyArgs a) {
     __syncthreads();
     if (tid == 0) {
         put(masses + blockIdx.x, (sums[0] + sums[1]) + (sums[2] + sums[3]));
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");            // waits for the store
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0): the store has been acknowledged before the arrival is counted
         last = (int)__hip_atomic_fetch_add(&a.decisions[r].arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
