@@ -211,3 +211,48 @@ def test_pool_beyond_4_gib(k):
     k.kvpr_paged_attention(desc, torch.from_numpy(q).cuda(), k.KVPR_F16, heads * d, pages, table, one(0, 1), one(300), 1, 1, 1, 300, z, heads * d, ws, ws.numel())
     torch.cuda.synchronize()
     assert np.array_equal(z.double().cpu().numpy(), small.attention(k, q))
+
+
+def test_many_requests(k):
+    """More requests than a workgroup has threads, most of them short: equal runs of the work, with many units each."""
+    rng = np.random.default_rng(15)
+    lens = rng.integers(1, 40, 700)
+    lens[[5, 300, 699]] = 900, 450, 130
+    new = np.minimum(rng.integers(0, 3, 700), lens)
+    b = Batch(lens, new, 2, 1, 64, 16, seed=15)
+    q = b.q("f16")
+    want = b.oracle(q)
+    for max_len in (900, 100000):
+        _check(b.attention(k, q, max_len=max_len), *want)
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,m", [(8, 8, 128, 1), (32, 8, 64, 7), (8, 8, 64, 3)])
+@pytest.mark.parametrize("q_type", ["f16", "f32"])
+def test_a_unit_for_each_workgroup(k, heads, kv_heads, d, m, q_type):
+    """Batches that fill the GPU with whole units (of several turns), and the same by runs, as a looser bound of the lengths gives."""
+    rng = np.random.default_rng(16)
+    lens = rng.integers(m, 300, 50)
+    b = Batch(lens, [m] * 50, heads, kv_heads, d, 16, seed=16)
+    q = b.q(q_type)
+    want = b.oracle(q)
+    _check(b.attention(k, q, max_len=300), *want)
+    _check(b.attention(k, q, max_len=100000), *want)
+
+
+@pytest.mark.parametrize("q_type", ["f16", "f32"])
+def test_many_rows_and_units(k, q_type):
+    """Rows of their own for each wave, a unit for each workgroup, against the launch that is made for few rows."""
+    b = Batch([500, 150, 333], [150, 150, 90], 64, 64, 64, 32, seed=17)
+    q = b.q(q_type)
+    z = b.attention(k, q)
+    few = b.attention(k, q, max_new=1, max_len=100000)
+    tol = 2.0 ** -10 * (np.abs(few) + 4.2)                              # twice the bound of either; no value is larger than 15 0.4 - 1.8
+    assert (np.abs(z - few) <= tol).all()
+    rows, heads = [0, 149, 150, 299, 300, 389], [0, 63]
+    sub = Batch([500, 150, 333], [150, 150, 90], 64, 64, 64, 32, seed=17)
+    for h in heads:
+        block = sub.page * 9 * sub.d // 8
+        one = sub.pages.reshape(sub.n_pages, 64, block)[:, h]
+        want, t, _ = po.attention(q[:, h * 64:(h + 1) * 64], one, sub.table, sub.row_start, sub.lens, 1, 1, 64, 32, q.shape[0])
+        got = z[:, h * 64:(h + 1) * 64]
+        assert (np.abs(got - want)[rows] <= t[rows]).all()

@@ -78,6 +78,16 @@ def test_verify(k, vocab, dtype, with_draft):
         _check(_run(k, target, draft, *rest, ld=ld), po.verify(target, draft, *rest, n_rows=target.shape[0]))
 
 
+@pytest.mark.parametrize("rows,vocab", [(200, 9001), (330, 9001), (6, 700001)])
+def test_sizes_of_chunks(k, rows, vocab):
+    """The first launch in chunks of 4096 and of 8192 logits, and a vocabulary of more chunks than a workgroup has threads."""
+    rng = np.random.default_rng(rows)
+    new = [3] * (rows // 3) + [1] * (rows % 3)
+    for dtype in (np.float16, np.float32):
+        target, draft, *rest = _inputs(rng, new, vocab, dtype)
+        _check(_run(k, target, draft, *rest), po.verify(target, draft, *rest, n_rows=target.shape[0]))
+
+
 @pytest.mark.parametrize("seed", range(20))
 def test_many_requests(k, seed):
     rng = np.random.default_rng(seed + 50)
