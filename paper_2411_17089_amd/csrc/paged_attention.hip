@@ -619,12 +619,12 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
 }
 
 // Joins the units of several workgroups: a wave has one row of the unit that workgroup x of the first launch left open, and asks for 16 of
-// its pieces at once, since what counts is the wait for them.
-constexpr int JOIN_ROWS = 16;           // of a workgroup: most have nothing to do, so there are few of them
+// its pieces at once, since what counts is the wait for them: 8 us for 64 units of 8 to 16 pieces and for 500 of 2 (four rows a wave
+// and four pieces at once 14 and 8, workgroups of 16 waves 11 and 11).
 template <int D>
-__global__ __launch_bounds__(JOIN_ROWS * 64) void paged_attention_join(const AttentionArgs a) {
+__global__ __launch_bounds__(NW * 64) void paged_attention_join(const AttentionArgs a) {
     constexpr int E = D / 64, U = 16;
-    const int lane = threadIdx.x & 63, row = blockIdx.y * JOIN_ROWS + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, row = blockIdx.y * NW + (threadIdx.x >> 6);
     const Open o = a.open[blockIdx.x];
     const int rr = o.row0 + row;
     if (o.pieces == 0 || rr >= o.real) return;
@@ -713,13 +713,13 @@ int launch_paged_attention(const PagedShape& s, const PagedAttention& x, void* w
     a.ldq = x.ldq; a.ldz = x.ldz;
     a.n = x.n; a.rows = x.rows; a.group = s.heads / s.kv_heads; a.slot_rows = c.slot_rows;
     a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)s.d));
-    const dim3 grid((unsigned)c.groups, c.direct ? (unsigned)x.n : 1), joined((unsigned)c.groups, (unsigned)(c.slot_rows / JOIN_ROWS));
+    const dim3 grid((unsigned)c.groups, c.direct ? (unsigned)x.n : 1), joined((unsigned)c.groups, (unsigned)(c.slot_rows / NW));
     auto launch = [&](auto kern) -> int {
         hipLaunchKernelGGL(kern, grid, dim3(NW * 64), 0, st, a);
         KVPR_HIP(hipGetLastError());
         if (c.direct) return KVPR_OK;
-        if (s.d == 128) hipLaunchKernelGGL(paged_attention_join<128>, joined, dim3(JOIN_ROWS * 64), 0, st, a);
-        else hipLaunchKernelGGL(paged_attention_join<64>, joined, dim3(JOIN_ROWS * 64), 0, st, a);
+        if (s.d == 128) hipLaunchKernelGGL(paged_attention_join<128>, joined, dim3(NW * 64), 0, st, a);
+        else hipLaunchKernelGGL(paged_attention_join<64>, joined, dim3(NW * 64), 0, st, a);
         KVPR_HIP(hipGetLastError());
         return KVPR_OK;
     };
