@@ -276,9 +276,11 @@ __device__ __forceinline__ int shares_of_chunk(const Shares<T>& s, int chunk, in
     return i;
 }
 
-// One workgroup per request: its rows joined, a wave per row and four rows at a time, up to the first draft that does not stand.
+// One workgroup per request: its rows joined, a wave per row and eight rows at a time, up to the first draft that does not stand
+// (five rows of 50272: 5.4 us, with four at a time 6.7; 64 requests of 32000: 6.2 and 9.1).
+constexpr int DECIDE_WAVES = 8;
 template <class T>
-__global__ __launch_bounds__(THREADS) void verify_decide(const VerifyArgs a) {
+__global__ __launch_bounds__(DECIDE_WAVES * 64) void verify_decide(const VerifyArgs a) {
     const Verify& v = a.v;
     __shared__ int stop, best;
     const int tid = threadIdx.x, wave = tid >> 6, r = blockIdx.x;
@@ -293,7 +295,7 @@ __global__ __launch_bounds__(THREADS) void verify_decide(const VerifyArgs a) {
         }
         return;
     }
-    for (int at = first;; at += WAVES) {
+    for (int at = first;; at += DECIDE_WAVES) {
         if (tid == 0) stop = end;
         __syncthreads();
         const int row = at + wave;
@@ -332,7 +334,7 @@ __global__ __launch_bounds__(THREADS) void verify_decide(const VerifyArgs a) {
         __syncthreads();
     }
     // the tokens; one that is drawn is put in its place by verify_draw
-    for (int i = first + tid; i < end; i += THREADS) v.out[i] = i < stop ? v.tokens[i + 1] : i == stop ? best : -1;
+    for (int i = first + tid; i < end; i += DECIDE_WAVES * 64) v.out[i] = i < stop ? v.tokens[i + 1] : i == stop ? best : -1;
 }
 
 // sum over the threads before this one; total: over all
@@ -493,7 +495,7 @@ int launch(const Verify& v, void* ws, hipStream_t st) {
         hipLaunchKernelGGL(stats, dim3((unsigned)(v.rows * l.chunks), v.draft ? 2 : 1), dim3(THREADS), 0, st, a);
         KVPR_HIP(hipGetLastError());
     }
-    hipLaunchKernelGGL(verify_decide<T>, dim3((unsigned)v.n), dim3(THREADS), 0, st, a);
+    hipLaunchKernelGGL(verify_decide<T>, dim3((unsigned)v.n), dim3(DECIDE_WAVES * 64), 0, st, a);
     KVPR_HIP(hipGetLastError());
     if (v.rows > 0) {
         hipLaunchKernelGGL(verify_draw<T>, dim3((unsigned)l.picks, (unsigned)v.n), dim3(THREADS), 0, st, a);
