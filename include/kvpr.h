@@ -458,7 +458,8 @@ int kvpr_dequant_int4(const void* src_dev, void* dst_dev, int64_t rows, int cols
  *
  * Rows.  The new tokens of all requests lie one behind the other: request r has rows row_start[r] .. row_start[r+1] - 1.  Every
  * row-wise call takes n_rows, the rows its arrays have; rows behind row_start[n_requests] are left as they were, and no
- * access goes past n_rows whatever row_start holds.
+ * access goes past n_rows whatever row_start holds.  n_rows (max_rows) is at most 2^30, in kvpr_paged_attention counted once for each
+ * query head of a key/value head.
  * Slots.  Position p of a request lies at slot = page * page_size + p % page_size, page = block_table[r][p / page_size].
  * Pages.  The pool is n_pages * kvpr_page_bytes bytes, 16-byte aligned.  The values are those of kvpr_quant_int4 (groups of 64 columns of
  * one head, (scale, minimum) in float16).  A page holds, for each key/value head, page_size * 9 * head_dim / 8 bytes:
@@ -468,7 +469,7 @@ int kvpr_dequant_int4(const void* src_dev, void* dst_dev, int64_t rows, int cols
  *     key pairs    [page_size][head_dim / 64] of (scale, minimum), then the value pairs likewise
  * with column 2 k in the low four bits of byte k, column 2 k + 1 in the high ones. */
 typedef struct {
-    int32_t n_heads;       /* query heads; query head i reads key/value head i / (n_heads / n_kv_heads) */
+    int32_t n_heads;       /* 1 to 16384; query head i reads key/value head i / (n_heads / n_kv_heads) */
     int32_t n_kv_heads;    /* divides n_heads                                                   */
     int32_t head_dim;      /* 64 or 128                                                         */
     int32_t page_size;     /* positions per page: 16, 32, 64, 128 or 256                        */
@@ -523,11 +524,12 @@ int kvpr_paged_attention(const kvpr_paged_desc* desc, const void* q, int q_type,
  *   draft x = tokens[row i + 1] stands if u_accept[row i + 1] q(x) < p(x); the first that does not ends the run;
  *   the next token is the first v with sum_{w <= v} s(w) > u_sample[r] sum_w s(w), s = max(p - q, 0) of the row that was rejected (p where that
  *   leaves nothing), s = p behind the last draft.  Shares and sums are evaluated in 64 bits.  u in [0, 1).
- * T <= 0 (or NaN): greedy, a draft stands if it is the row's largest logit (lowest index on ties), and the next token is the largest one.
+ * T above 10^30 counts as 10^30.  T <= 0 (or NaN): greedy, a draft stands if it is the row's largest logit (lowest index on ties), and the next token is the largest one.
  * Out: out_tokens of a request's rows: the drafts that stand, the next token, -1 for the rest; kept[r] = rows of the cache that stay = tokens gained
  * (0 for a request without rows); len_out[r] = len_in[r] + kept[r] (both null: not wanted; the same array is allowed): with len_in = base_len, the next plan's base_len.
  * A logit of NaN counts as -inf.  A target row of nothing but -inf has no distribution: the run ends there, and the next token is -1.  A draft outside
- * [0, vocab) does not stand.  ws: 16-byte aligned, kvpr_verify_workspace_bytes bytes.  vocab at most 2^24. */
+ * [0, vocab) does not stand.  ws: 16-byte aligned, kvpr_verify_workspace_bytes bytes.  vocab at most 2^24,
+ * n_rows * ceil(vocab / 2048) below 2^23. */
 size_t kvpr_verify_workspace_bytes(int n_requests, int n_rows, int vocab);
 int kvpr_verify_drafts(const void* target_logits, const void* draft_logits, int logits_type, int64_t ld_target, int64_t ld_draft, int vocab,
                        const int32_t* tokens, const int32_t* row_start, int n_requests, int n_rows, const float* temperature,

@@ -5,6 +5,8 @@ using kvpr::fail;
 
 namespace {
 
+constexpr int MOST_ROWS = 1 << 30;      // row numbers and what is added to them stay in 32 bits
+
 int log2_of(int v) {
     int l = 0;
     while ((1 << l) < v) ++l;
@@ -14,7 +16,7 @@ int log2_of(int v) {
 int check_shape(const kvpr_paged_desc* d, kvpr::PagedShape& s) {
     if (!d) return fail(KVPR_E_INVAL, "desc is null");
     if (d->head_dim != 64 && d->head_dim != 128) return fail(KVPR_E_INVAL, "head_dim must be 64 or 128");
-    if (d->n_heads < 1 || d->n_kv_heads < 1 || d->n_heads > 65535) return fail(KVPR_E_RANGE, "n_heads=%d n_kv_heads=%d out of range", d->n_heads, d->n_kv_heads);
+    if (d->n_heads < 1 || d->n_kv_heads < 1 || d->n_heads > 16384) return fail(KVPR_E_RANGE, "n_heads=%d n_kv_heads=%d out of range", d->n_heads, d->n_kv_heads);
     if (d->n_heads % d->n_kv_heads) return fail(KVPR_E_INVAL, "n_kv_heads=%d does not divide n_heads=%d", d->n_kv_heads, d->n_heads);
     if (d->page_size < 16 || d->page_size > 256 || (d->page_size & (d->page_size - 1)))
         return fail(KVPR_E_INVAL, "page_size=%d must be 16, 32, 64, 128 or 256", d->page_size);
@@ -38,8 +40,8 @@ extern "C" int kvpr_paged_plan(const kvpr_paged_desc* desc, const int32_t* base_
                                int max_rows, int32_t* row_start, int32_t* seq_len, int32_t* slots, int32_t* positions, int32_t* refused, void* stream) {
     kvpr::PagedShape s;
     if (int rc = check_shape(desc, s)) return rc;
-    if (n_requests < 1 || n_requests > kvpr::kMaxRequests || max_rows < 0)
-        return fail(KVPR_E_RANGE, "n_requests=%d (1 to %d) max_rows=%d out of range", n_requests, kvpr::kMaxRequests, max_rows);
+    if (n_requests < 1 || n_requests > kvpr::kMaxRequests || max_rows < 0 || max_rows > MOST_ROWS)
+        return fail(KVPR_E_RANGE, "n_requests=%d (1 to %d) max_rows=%d (0 to 2^30) out of range", n_requests, kvpr::kMaxRequests, max_rows);
     if (!base_len || !new_len || !block_table || !held_in || !held_out || !free_pages || !free_count_in || !free_count_out || !row_start || !seq_len || !refused)
         return fail(KVPR_E_INVAL, "null pointer");
     if (max_rows > 0 && (!slots || !positions)) return fail(KVPR_E_INVAL, "slots / positions is null");
@@ -52,7 +54,7 @@ extern "C" int kvpr_paged_append(const kvpr_paged_desc* desc, const void* qkv, i
                                  const void* rope_table, int n_pos, void* q_out, int64_t ldq, void* pages, void* stream) {
     kvpr::PagedShape s;
     if (int rc = check_shape(desc, s)) return rc;
-    if (n_rows < 0) return fail(KVPR_E_RANGE, "n_rows=%d out of range", n_rows);
+    if (n_rows < 0 || n_rows > MOST_ROWS) return fail(KVPR_E_RANGE, "n_rows=%d (0 to 2^30) out of range", n_rows);
     const int64_t q_cols = (int64_t)s.heads * s.d, cols = q_cols + 2 * (int64_t)s.kv_heads * s.d;
     if (ld < cols || ld % 8) return fail(KVPR_E_INVAL, "need ld >= %lld, ld %% 8 == 0 (16-byte row pieces)", (long long)cols);
     if (rope_table && n_pos < 1) return fail(KVPR_E_RANGE, "n_pos=%d out of range", n_pos);
@@ -67,7 +69,7 @@ extern "C" int kvpr_paged_append(const kvpr_paged_desc* desc, const void* qkv, i
 extern "C" int kvpr_paged_read(const kvpr_paged_desc* desc, const void* pages, const int32_t* slots, int n_rows, void* kv, int64_t ld, void* stream) {
     kvpr::PagedShape s;
     if (int rc = check_shape(desc, s)) return rc;
-    if (n_rows < 0) return fail(KVPR_E_RANGE, "n_rows=%d out of range", n_rows);
+    if (n_rows < 0 || n_rows > MOST_ROWS) return fail(KVPR_E_RANGE, "n_rows=%d (0 to 2^30) out of range", n_rows);
     const int64_t cols = 2 * (int64_t)s.kv_heads * s.d;
     if (ld < cols || ld % 8) return fail(KVPR_E_INVAL, "need ld >= %lld, ld %% 8 == 0 (16-byte row pieces)", (long long)cols);
     if (n_rows == 0) return KVPR_OK;
@@ -95,7 +97,7 @@ extern "C" int kvpr_paged_attention(const kvpr_paged_desc* desc, const void* q, 
     if (int rc = check_shape(desc, s)) return rc;
     if (int rc = check_batch(n_requests, n_rows, max_new, max_len)) return rc;
     if (q_type != KVPR_F16 && q_type != KVPR_F32) return fail(KVPR_E_INVAL, "q_type must be KVPR_F16 or KVPR_F32");
-    if ((int64_t)n_rows * (s.heads / s.kv_heads) > (1 << 30)) return fail(KVPR_E_RANGE, "n_rows=%d times %d heads per key/value head is beyond 2^30", n_rows, s.heads / s.kv_heads);
+    if ((int64_t)n_rows * (s.heads / s.kv_heads) > MOST_ROWS) return fail(KVPR_E_RANGE, "n_rows=%d times %d heads per key/value head is beyond 2^30", n_rows, s.heads / s.kv_heads);
     const int64_t cols = (int64_t)s.heads * s.d;
     if (ldq < cols || ldq % 8 || ldz < cols || ldz % 8) return fail(KVPR_E_INVAL, "need ldq, ldz >= %lld and multiples of 8", (long long)cols);
     if (n_rows == 0) return KVPR_OK;

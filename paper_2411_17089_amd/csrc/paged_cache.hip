@@ -155,50 +155,50 @@ __global__ __launch_bounds__(WAVES * 64) void paged_append_kernel(PagedShape s, 
     half8 ahead[AHEAD];
     for (int unit = unit0; unit < min(unit0 + HEADS, units); unit += AHEAD) {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) ahead[i] = load_unit(part_of(unit + i));
+        for (int i = 0; i < AHEAD; ++i) ahead[i] = load_unit(part_of(unit + i));
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-        const Part part = part_of(unit + i);
-        half8 here = ahead[i];
-        const bool exists = part.exists, is_q = part.is_q, is_k = part.is_k;
-        const int head = part.head;
-        if (is_q || is_k) {
-            if (rope) here = rotate<D>(here, rope, position, j);
-            if (is_q) {
-                if (turned) *reinterpret_cast<half8*>(q_out + row * ldq + (int64_t)head * D + j * 8) = here;
-                continue;
-            }
-            const Packed p = pack(here);
-            if (slot < 0 || !exists) continue;
-            const int t = slot & (s.page - 1);
-            uint8_t* block = pages + (int64_t)(slot >> s.page_log2) * s.page_bytes() + (int64_t)head * s.block_bytes();
-            *reinterpret_cast<uint32_t*>(block + t * (D / 2) + key_place<D>(4 * j)) = p.codes;
-            if ((j & 7) == 0) *reinterpret_cast<uint32_t*>(block + s.page * D + (t * NG + (j >> 3)) * 4) = p.pair;
-            continue;
-        }
-        // values: the quad that starts here, then rows that are in none
-        if (lead >= 0) {
-            const Packed p = pack(here);
-            const uint32_t word = turn_over(p.codes);
-            const int t = (lead_slot & (s.page - 1)) + sub;
-            uint8_t* block = pages + (int64_t)(lead_slot >> s.page_log2) * s.page_bytes() + (int64_t)head * s.block_bytes();
-            if (exists) {
-                *reinterpret_cast<uint32_t*>(block + s.page * (D / 2) + (t >> 2) * (2 * D) + value_place<D>(4 * j + sub) * 4) = word;
-                if ((j & 7) == 0) *reinterpret_cast<uint32_t*>(block + s.page * D + s.page * (NG * 4) + (t * NG + (j >> 3)) * 4) = p.pair;
-            }
-        }
-        if (__any(alone)) {
-            const Packed p = pack(lead >= 0 ? load(part, row, alone) : here);
-            if (alone && exists) {
+        for (int i = 0; i < AHEAD; ++i) {
+            const Part part = part_of(unit + i);
+            half8 here = ahead[i];
+            const bool exists = part.exists, is_q = part.is_q, is_k = part.is_k;
+            const int head = part.head;
+            if (is_q || is_k) {
+                if (rope) here = rotate<D>(here, rope, position, j);
+                if (is_q) {
+                    if (turned) *reinterpret_cast<half8*>(q_out + row * ldq + (int64_t)head * D + j * 8) = here;
+                    continue;
+                }
+                const Packed p = pack(here);
+                if (slot < 0 || !exists) continue;
                 const int t = slot & (s.page - 1);
                 uint8_t* block = pages + (int64_t)(slot >> s.page_log2) * s.page_bytes() + (int64_t)head * s.block_bytes();
+                *reinterpret_cast<uint32_t*>(block + t * (D / 2) + key_place<D>(4 * j)) = p.codes;
+                if ((j & 7) == 0) *reinterpret_cast<uint32_t*>(block + s.page * D + (t * NG + (j >> 3)) * 4) = p.pair;
+                continue;
+            }
+            // values: the quad that starts here, then rows that are in none
+            if (lead >= 0) {
+                const Packed p = pack(here);
+                const uint32_t word = turn_over(p.codes);
+                const int t = (lead_slot & (s.page - 1)) + sub;
+                uint8_t* block = pages + (int64_t)(lead_slot >> s.page_log2) * s.page_bytes() + (int64_t)head * s.block_bytes();
+                if (exists) {
+                    *reinterpret_cast<uint32_t*>(block + s.page * (D / 2) + (t >> 2) * (2 * D) + value_place<D>(4 * j + sub) * 4) = word;
+                    if ((j & 7) == 0) *reinterpret_cast<uint32_t*>(block + s.page * D + s.page * (NG * 4) + (t * NG + (j >> 3)) * 4) = p.pair;
+                }
+            }
+            if (__any(alone)) {
+                const Packed p = pack(lead >= 0 ? load(part, row, alone) : here);
+                if (alone && exists) {
+                    const int t = slot & (s.page - 1);
+                    uint8_t* block = pages + (int64_t)(slot >> s.page_log2) * s.page_bytes() + (int64_t)head * s.block_bytes();
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    block[s.page * (D / 2) + (t >> 2) * (2 * D) + value_place<D>(4 * j + i) * 4 + (t & 3)] = (uint8_t)(p.codes >> (8 * i));
-                if ((j & 7) == 0) *reinterpret_cast<uint32_t*>(block + s.page * D + s.page * (NG * 4) + (t * NG + (j >> 3)) * 4) = p.pair;
+                    for (int i = 0; i < 4; ++i)
+                        block[s.page * (D / 2) + (t >> 2) * (2 * D) + value_place<D>(4 * j + i) * 4 + (t & 3)] = (uint8_t)(p.codes >> (8 * i));
+                    if ((j & 7) == 0) *reinterpret_cast<uint32_t*>(block + s.page * D + s.page * (NG * 4) + (t * NG + (j >> 3)) * 4) = p.pair;
+                }
             }
         }
-    }
     }
 }
 

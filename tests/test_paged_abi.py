@@ -9,7 +9,7 @@ def k():
 
 
 GOOD = dict(n_heads=8, n_kv_heads=2, head_dim=128, page_size=16, n_pages=4, table_width=4)
-BAD = [(dict(head_dim=96), "E_INVAL"), (dict(n_heads=0), "E_RANGE"), (dict(n_heads=70000, n_kv_heads=70000), "E_RANGE"), (dict(n_kv_heads=0), "E_RANGE"),
+BAD = [(dict(head_dim=96), "E_INVAL"), (dict(n_heads=0), "E_RANGE"), (dict(n_heads=70000, n_kv_heads=70000), "E_RANGE"), (dict(n_heads=16385, n_kv_heads=1), "E_RANGE"), (dict(n_kv_heads=0), "E_RANGE"),
        (dict(n_kv_heads=3), "E_INVAL"), (dict(page_size=8), "E_INVAL"), (dict(page_size=48), "E_INVAL"), (dict(page_size=512), "E_INVAL"),
        (dict(n_pages=0), "E_RANGE"), (dict(n_pages=1 << 27), "E_RANGE"), (dict(table_width=0), "E_RANGE"), (dict(table_width=1 << 27), "E_RANGE")]
 
@@ -44,7 +44,8 @@ def test_bad_descriptions(k, change, code):
 
 
 # call, argument, value, code
-ARGS = [("plan", 3, 0, "E_RANGE"), ("plan", 3, 8193, "E_RANGE"), ("plan", 10, -1, "E_RANGE")] + \
+ARGS = [("plan", 3, 0, "E_RANGE"), ("plan", 3, 8193, "E_RANGE"), ("plan", 10, -1, "E_RANGE"), ("plan", 10, (1 << 30) + 1, "E_RANGE"), ("append", 5, (1 << 30) + 1, "E_RANGE"),
+        ("read", 3, (1 << 30) + 1, "E_RANGE"), ("attention", 9, (1 << 28) + 1, "E_RANGE"), ("verify", 9, 1 << 23, "E_RANGE")] + \
        [("plan", i, None, "E_INVAL") for i in (1, 2, 4, 5, 6, 7, 8, 9, 11, 12, 13, 14, 15)] + \
        [("append", 2, 1528, "E_INVAL"), ("append", 2, 1540, "E_INVAL"), ("append", 5, -1, "E_RANGE"), ("append", 7, 0, "E_RANGE"), ("append", 6, None, "E_INVAL"),
         ("append", 9, 1016, "E_INVAL"), ("append", 9, 1028, "E_INVAL"), ("append", 1, (1 << 20) + 8, "E_INVAL"), ("append", 8, (1 << 20) + 2, "E_INVAL"),
