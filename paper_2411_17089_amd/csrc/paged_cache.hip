@@ -16,12 +16,12 @@ namespace kvpr {
 namespace {
 
 // float64 -> float16 in one rounding: the float32 between is made odd in its last bit where it is inexact, and an odd one is
-// neither a float16 nor the middle between two
+// neither a float16 nor the middle between two.  Zeros (of less than half the smallest float32) and infinities (whose rest is NaN) stay
 __device__ __forceinline__ _Float16 to_half(double x) {
     float f = (float)x;
     const double rest = x - (double)f;
     int bits = __float_as_int(f);
-    if (rest != 0.0 && !(bits & 1)) bits += (rest > 0.0) == (f > 0.f) ? 1 : -1;
+    if (fabs(rest) > 0.0 && f != 0.f && !(bits & 1)) bits += (rest > 0.0) == (f > 0.f) ? 1 : -1;
     return (_Float16)__int_as_float(bits);
 }
 

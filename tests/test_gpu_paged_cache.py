@@ -169,3 +169,21 @@ def test_pool_beyond_4_gib(k):
     want = io.roundtrip(x[:, 64 * d:].cpu().numpy())
     assert np.array_equal(out.cpu().numpy().view(np.uint16), want.view(np.uint16))
     assert int((pages[1:n_pages - 1] != 0).sum()) == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_rotation_of_infinities_and_to_nothing(k, d):
+    """q with infinities keeps their signs; angles whose products are below the smallest float32 give zeros of the right sign."""
+    page, rows = 16, 8
+    x = np.random.default_rng(2).standard_normal((rows, 3 * d)).astype(np.float16)
+    x[0, 3], x[1, 3], x[2, d // 2 + 5], x[3, d - 1] = np.inf, -np.inf, np.inf, -np.inf
+    x[4, 0], x[4, d // 2], x[5, 1] = np.inf, -np.inf, np.nan
+    x[6:] = np.float16(2.0 ** -24) * np.where(np.arange(3 * d) % 3 == 0, -1, 1).astype(np.float16)
+    table = np.concatenate([k.kvpr_rope_table(6, d), np.full((2, d // 2, 2), 1e-45, np.float32)])
+    positions = np.array([1, 2, 3, 4, 5, 0, 6, 7])
+    _, q = _append(k, x, np.arange(rows), positions, 1, 1, d, page, 1, table)
+    with np.errstate(all="ignore"):
+        want = po.rotate(x.reshape(rows, 3, d)[:, :1], table, positions).astype(np.float16).reshape(rows, d)
+    assert (np.isinf(want) & (want < 0)).any() and (np.isinf(want) & (want > 0)).any() and (want[6:] == 0).all()
+    assert np.array_equal(np.isnan(q), np.isnan(want))
+    assert np.array_equal(q.view(np.uint16)[~np.isnan(want)], want.view(np.uint16)[~np.isnan(want)])
