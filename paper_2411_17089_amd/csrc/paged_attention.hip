@@ -80,8 +80,9 @@ struct AttentionArgs {
     int n, rows, group, slot_rows;
     float scale_log2;
 };
-// the unit that a workgroup began and left to those behind it: pieces = 0: none
-struct Open { int pieces, first, row0, real, kv_head; };
+// the unit that a workgroup began and left to those behind it, rows row0 .. end - 1 (fewer than slot_rows where the waves share them while
+// other requests' units have more); pieces = 0: none
+struct Open { int pieces, first, row0, end, kv_head; };
 constexpr int FEW = 64;                 // rows up to which a workgroup's waves share them
 constexpr int START = 3;                // what a unit costs beside its turns, in turns: lengths, queries, first operands, the join of the waves
 
@@ -552,7 +553,7 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
         for (int mt = 0; mt < MT; ++mt) l[mt] = across_rows(l[mt], sum_of);
         const bool all_here = DIRECT || (turn0 == 0 && turn1 == rq.turns);
         if (!all_here && turn0 == 0 && threadIdx.x == 0)    // the rest of the turns end in the workgroup that has the last of them
-            a.open[b] = Open{(int)(group_of(at + (rq.turns - turn1) - 1, groups, total) - b) + 1, rq.first, row0, rq.real, kv_head};
+            a.open[b] = Open{(int)(group_of(at + (rq.turns - turn1) - 1, groups, total) - b) + 1, rq.first, row0, min(rq.real, row0 + rq.tile_rows), kv_head};
         float* slot = a.part + ((b * 2 + (turn0 == 0)) * a.slot_rows + region * (MT * 16)) * (D + 2);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
@@ -627,7 +628,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_join(const AttentionA
     const int lane = threadIdx.x & 63, row = blockIdx.y * NW + (threadIdx.x >> 6);
     const Open o = a.open[blockIdx.x];
     const int rr = o.row0 + row;
-    if (o.pieces == 0 || rr >= o.real) return;
+    if (o.pieces == 0 || rr >= o.end) return;
     const int64_t stride = 2 * (int64_t)a.slot_rows * (D + 2);
     const float* from = a.part + blockIdx.x * stride + (int64_t)row * (D + 2);          // slot 1 of the first, slot 0 of those behind it
     float top = LOWEST, l = 0.f, sum[E] = {};
