@@ -509,6 +509,8 @@ int kvpr_paged_read(const kvpr_paged_desc* desc, const void* pages, const int32_
  * included), row i of request r sees positions [0, seq_len[r] - m + i + 1): z = softmax(q k^T / sqrt(head_dim)) v in float16, row stride ldz.
  * A row that sees nothing gives 0.  k is code * scale + minimum, v that rounded to float16 as kvpr_dequant_int4 gives it.  Positions whose table entry lies
  * outside the pool, or behind table_width entries, take no part.
+ * Values that are not finite (scales, minima, or 15 scale + minimum beyond float16's range) leave rows that do not see their position as they are; rows that do
+ * are not finite in the columns of those values, and may be NaN in their other columns too.
  * q: KVPR_F16 or KVPR_F32, row stride ldq (elements).  max_new and max_len: how many new tokens and positions a request has at most,
  * as far as the host knows; they size the launch and the workspace, and results are right for requests beyond them too.
  * ldq, ldz % 8 == 0; q, pages, z, ws 16-byte aligned; ws needs kvpr_paged_attention_workspace_bytes of the same arguments. */

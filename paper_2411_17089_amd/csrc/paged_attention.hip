@@ -441,11 +441,12 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
 #pragma unroll
                     for (int p = 0; p < 4; ++p) {
                         const int t = t0 + 16 * u + 4 * g + p;
-                        float poison = 0.f;                             // NaN for values that are not finite
+                        float poison = 0.f;                             // NaN for values that are not finite, or whose largest passes float16 where not all rows see it
 #pragma unroll
                         for (int gr = 0; gr < NG; ++gr) {
                             const half2v sm = vm[u].at(p, gr);
                             poison += (float)sm[0] * 0.f + (float)sm[1] * 0.f;
+                            if (t >= all_see) poison += (float)(_Float16)fmaf((float)sm[0], 15.f, (float)sm[1]) * 0.f;
                         }
                         // positions that a row does not see must not reach its sum, not even as 0 times NaN
                         const bool out = t >= all || poison != 0.f;
