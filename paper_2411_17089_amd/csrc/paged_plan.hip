@@ -4,7 +4,7 @@
 // The work is a chain of latencies, not of bytes: three prefix sums over the requests (pages given back, pages taken, rows) in one
 // pass of one workgroup, then the pages, a thread each whatever request they belong to (a thread per request walked up to 128 pages
 // one by one), then the new tokens, a thread each: by the same workgroup, or, where they are many, by a launch of their own.
-// 512 requests, 31500 new tokens: 88 us by one workgroup with searches in global memory.
+// 8 requests 4.6 us; 512 requests, 31500 new tokens 8.3 and 4.4 us, 88 by one workgroup with searches in global memory.
 #include "paged.h"
 
 namespace kvpr {
