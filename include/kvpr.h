@@ -53,7 +53,7 @@ extern "C" {
 #define KVPR_E_STATE  -5   /* call not valid in the current state (e.g. rows unwritten) */
 
 #define KVPR_F16 1
-#define KVPR_F32 2   /* where an entry point takes a type: q of kvpr_paged_attention, logits of kvpr_verify_drafts */
+#define KVPR_F32 2   /* where an entry point takes a type: q of kvpr_paged_attention, logits of kvpr_verify_step */
 /* Flags or-ed into kvpr_model_desc.dtype: keep the host store group-wise 4-bit compressed
  * (Sec. 4.4 "KV Cache Compression").  KV_INT4 compresses the cache rows, X_INT4 the stored
  * activations; KVPR_STORE_INT4 sets both.  All arithmetic stays float16 / float32: activation rows
@@ -451,7 +451,7 @@ int kvpr_dequant_int4(const void* src_dev, void* dst_dev, int64_t rows, int cols
  *     kvpr_paged_plan       pages, row offsets, slots and positions of the new tokens, from the lengths
  *     kvpr_paged_append     per layer: rotate, pack the new tokens' k and v into their slots
  *     kvpr_paged_attention  per layer: the new tokens over the pages
- *     kvpr_verify_drafts    which drafts stand, the token behind them, and the lengths that the next plan starts from
+ *     kvpr_verify_step      which drafts stand, the token behind them, and the lengths that the next plan starts from
  * Lengths, tables and decisions stay on the device: no call waits, allocates or reads device memory from the host, so a step can be captured into a
  * graph.  All arrays are device arrays, and calls that share written arrays or a workspace must run one after the
  * other.  Arrays of one call must not overlap unless the text allows it.
@@ -537,6 +537,13 @@ int kvpr_verify_drafts(const void* target_logits, const void* draft_logits, int 
                        const int32_t* tokens, const int32_t* row_start, int n_requests, int n_rows, const float* temperature,
                        const float* u_accept, const float* u_sample, const int32_t* len_in, int32_t* len_out, int32_t* kept,
                        int32_t* out_tokens, void* ws, size_t ws_bytes, void* stream);
+/* kvpr_verify_drafts takes every request that has rows for one whose rows were appended and attended, so it is for steps in which the plan refuses
+ * nobody.  kvpr_verify_step takes the plan's seq_len as well: a request with rows and seq_len[r] <= 0 was refused.  Its logits are not read, its tokens are -1, kept[r] = 0 and
+ * len_out[r] = len_in[r], so that the same tokens can be brought again.  seq_len null: as kvpr_verify_drafts. */
+int kvpr_verify_step(const void* target_logits, const void* draft_logits, int logits_type, int64_t ld_target, int64_t ld_draft, int vocab,
+                     const int32_t* tokens, const int32_t* row_start, const int32_t* seq_len, int n_requests, int n_rows,
+                     const float* temperature, const float* u_accept, const float* u_sample, const int32_t* len_in, int32_t* len_out,
+                     int32_t* kept, int32_t* out_tokens, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

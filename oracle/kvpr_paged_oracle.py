@@ -172,13 +172,17 @@ def _share(logits, t):
     return e / e.sum()
 
 
-def verify(target, draft, tokens, row_start, temperature, u_accept, u_sample, n_rows):
-    """-> (out_tokens, kept); rows outside every request are given as None."""
+def verify(target, draft, tokens, row_start, temperature, u_accept, u_sample, n_rows, seq_len=None):
+    """-> (out_tokens, kept); rows outside every request are given as None.  A request whose seq_len is 0 was refused: nothing of it counts."""
     out, kept = [None] * n_rows, []
     vocab = target.shape[1]
     for r in range(len(row_start) - 1):
         a, b = int(row_start[r]), min(int(row_start[r + 1]), n_rows)
         if a >= b:
+            kept.append(0)
+            continue
+        if seq_len is not None and seq_len[r] <= 0:
+            out[a:b] = [-1] * (b - a)
             kept.append(0)
             continue
         t = float(temperature[r])

@@ -1,4 +1,5 @@
-// Verification of drafted tokens against the target's probabilities, from given random numbers (formulas at kvpr_verify_drafts).
+// Verification of drafted tokens against the target's probabilities, from given random numbers (formulas at kvpr_verify_drafts; kvpr_verify_step is the
+// same behind a plan that may have refused requests).
 //
 // Three launches over chunks of the vocabulary, since the order of a request's steps leaves one workgroup per request otherwise
 // (five rows of 50272: 226 us in one workgroup):
@@ -153,6 +154,7 @@ __global__ __launch_bounds__(THREADS) void verify_stats(const VerifyArgs a) {
     for (int w = 0; w < WAVES; ++w) owner += counts[w];
     const int first = v.row_start[owner];
     if (row >= v.row_start[owner + 1] || row < first || (side && row == first)) return;
+    if (v.seq_len && v.seq_len[owner] <= 0) return;
     const double inv_t = inverse(v.temperature[owner]);
     // the elements that are no whole piece of 8: at most 7, one a thread
     const int tail = n & ~7;
@@ -287,12 +289,14 @@ __global__ __launch_bounds__(DECIDE_WAVES * 64) void verify_decide(const VerifyA
     const int first = max(v.row_start[r], 0), end = min(v.row_start[r + 1], v.rows);
     const double inv_t = inverse(v.temperature[r]);
     const bool greedy = inv_t == 0.0;
-    if (first >= end) {
+    // no rows, or refused by the plan: its rows have no slots, so no attention and no logits stand behind them
+    if (first >= end || (v.seq_len && v.seq_len[r] <= 0)) {
         if (tid == 0) {
             v.kept[r] = 0;
             if (v.len_out) v.len_out[r] = v.len_in[r];
             a.decisions[r].row = -1;
         }
+        for (int i = first + tid; i < end; i += DECIDE_WAVES * 64) v.out[i] = -1;
         return;
     }
     for (int at = first;; at += DECIDE_WAVES) {
