@@ -521,7 +521,7 @@ int kvpr_paged_attention(const kvpr_paged_desc* desc, const void* q, int q_type,
 
 /* Verification of drafts.  Row 0 of a request is its last certain token, rows 1 .. m - 1 are drafts; tokens[] holds what was fed, target_logits
  * [n_rows, vocab] (KVPR_F16 or KVPR_F32, row strides in elements) what the target model says after each row, draft_logits the distribution that the draft
- * in the SAME row was drawn from (row 0's is not read); null: the drafts come without probabilities (a lookup), q = 1 at the draft.
+ * in the SAME row was drawn from (row 0's is not read, nor are rows behind the last request's, so neither need be there); null: the drafts come without probabilities (a lookup), q = 1 at the draft.
  *   p = softmax(target row i / T), q = softmax(draft row i + 1 / T), T = temperature[r];
  *   draft x = tokens[row i + 1] stands if u_accept[row i + 1] q(x) < p(x); the first that does not ends the run;
  *   the next token is the first v with sum_{w <= v} s(w) > u_sample[r] sum_w s(w), s = max(p - q, 0) of the row that was rejected (p where that

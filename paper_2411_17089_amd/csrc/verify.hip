@@ -139,15 +139,18 @@ __global__ __launch_bounds__(THREADS) void verify_stats(const VerifyArgs a) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) count += __shfl_xor(count, o);
     if ((tid & 63) == 0) counts[tid >> 6] = count;
-    // the row is asked for meanwhile
     const T* from = (side ? (const T*)v.draft + row * v.ld_draft : (const T*)v.target + row * v.ld_target) + (int64_t)chunk * a.chunk;
     const int n = min(a.chunk, v.vocab - chunk * a.chunk);
     Eight<T> x[E / 8];
+    auto ask = [&] {
 #pragma unroll
-    for (int j = 0; j < E / 8; ++j) {
-        const int i = (j * THREADS + tid) * 8;
-        if (i + 8 <= n) x[j].load(from + i);
-    }
+        for (int j = 0; j < E / 8; ++j) {
+            const int i = (j * THREADS + tid) * 8;
+            if (i + 8 <= n) x[j].load(from + i);
+        }
+    };
+    // a row of the target is asked for meanwhile; one of the draft only once it is known to be no request's first, which need not be there
+    if (!side) ask();
     __syncthreads();
     int owner = 0;
 #pragma unroll
@@ -155,6 +158,7 @@ __global__ __launch_bounds__(THREADS) void verify_stats(const VerifyArgs a) {
     const int first = v.row_start[owner];
     if (row >= v.row_start[owner + 1] || row < first || (side && row == first)) return;
     if (v.seq_len && v.seq_len[owner] <= 0) return;
+    if (side) ask();
     const double inv_t = inverse(v.temperature[owner]);
     // the elements that are no whole piece of 8: at most 7, one a thread
     const int tail = n & ~7;
