@@ -537,12 +537,17 @@ int kvpr_verify_drafts(const void* target_logits, const void* draft_logits, int 
                        const int32_t* tokens, const int32_t* row_start, int n_requests, int n_rows, const float* temperature,
                        const float* u_accept, const float* u_sample, const int32_t* len_in, int32_t* len_out, int32_t* kept,
                        int32_t* out_tokens, void* ws, size_t ws_bytes, void* stream);
-/* kvpr_verify_drafts takes every request that has rows for one whose rows were appended and attended, so it is for steps in which the plan refuses
- * nobody.  kvpr_verify_step takes the plan's seq_len as well: a request with rows and seq_len[r] <= 0 was refused.  Its logits are not read, its tokens are -1, kept[r] = 0 and
- * len_out[r] = len_in[r], so that the same tokens can be brought again.  seq_len null: as kvpr_verify_drafts. */
+/* kvpr_verify_drafts takes every request that has rows for one whose rows were appended and attended, and all rows but its first for drafts: it is for
+ * steps in which the plan refuses nobody and no prompt comes in.  kvpr_verify_step takes two more arrays; with both null it is kvpr_verify_drafts.
+ *   seq_len  the plan's: a request with rows and seq_len[r] <= 0 was refused.  Its logits count for nothing, its tokens are -1, kept[r] = 0 and len_out[r] = len_in[r],
+ *            so that the same tokens can be brought again.
+ *   certain  how many of a request's rows, from its first on, are certain tokens (a prompt chunk, or the last token alone: 1); less than 1 counts as 1, more than its
+ *            rows as all.  A certain token stands whatever the logits say: out_tokens of the row in front of it is that token, and its row is kept.  Drafts begin
+ *            behind the last certain row, and the next token comes from there on as above: of a prompt's last chunk it is the first of the answer, of
+ *            the chunks in front of it the caller knows better.  Only the target's rows from the last certain one on and the drafts' rows take part. */
 int kvpr_verify_step(const void* target_logits, const void* draft_logits, int logits_type, int64_t ld_target, int64_t ld_draft, int vocab,
-                     const int32_t* tokens, const int32_t* row_start, const int32_t* seq_len, int n_requests, int n_rows,
-                     const float* temperature, const float* u_accept, const float* u_sample, const int32_t* len_in, int32_t* len_out,
+                     const int32_t* tokens, const int32_t* row_start, const int32_t* seq_len, const int32_t* certain, int n_requests,
+                     int n_rows, const float* temperature, const float* u_accept, const float* u_sample, const int32_t* len_in, int32_t* len_out,
                      int32_t* kept, int32_t* out_tokens, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus

@@ -172,8 +172,9 @@ def _share(logits, t):
     return e / e.sum()
 
 
-def verify(target, draft, tokens, row_start, temperature, u_accept, u_sample, n_rows, seq_len=None):
-    """-> (out_tokens, kept); rows outside every request are given as None.  A request whose seq_len is 0 was refused: nothing of it counts."""
+def verify(target, draft, tokens, row_start, temperature, u_accept, u_sample, n_rows, seq_len=None, certain=None):
+    """-> (out_tokens, kept); rows outside every request are given as None.  A request whose seq_len is 0 was refused: nothing of it counts.
+    certain: rows of each request, from its first on, that hold certain tokens; a token that is certain stands."""
     out, kept = [None] * n_rows, []
     vocab = target.shape[1]
     for r in range(len(row_start) - 1):
@@ -188,7 +189,12 @@ def verify(target, draft, tokens, row_start, temperature, u_accept, u_sample, n_
         t = float(temperature[r])
         greedy = not t > 0
         row, pick = a, None
+        sure = a + (1 if certain is None else max(int(certain[r]), 1))
         while pick is None:
+            if row + 1 < min(sure, b):
+                out[row] = int(tokens[row + 1])
+                row += 1
+                continue
             x = int(tokens[row + 1]) if row + 1 < b else None
             p = _share(target[row], 1.0 if greedy else t)
             ok = False

@@ -123,7 +123,7 @@ _SIGS = {
     "kvpr_paged_attention": (_i, [_vp, _vp, _i, _i64, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _i64, _vp, _sz, _vp]),
     "kvpr_verify_workspace_bytes": (_sz, [_i, _i, _i]),
     "kvpr_verify_drafts": (_i, [_vp, _vp, _i, _i64, _i64, _i, _vp, _vp, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
-    "kvpr_verify_step": (_i, [_vp, _vp, _i, _i64, _i64, _i, _vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "kvpr_verify_step": (_i, [_vp, _vp, _i, _i64, _i64, _i, _vp, _vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
 }
 EXPORTS = tuple(_SIGS)
 for _name, (_res, _args) in _SIGS.items():
@@ -500,12 +500,12 @@ def kvpr_verify_drafts(target_logits, draft_logits, logits_type, ld_target, ld_d
                                   kp, out, ws, ws_bytes, _current(d, stream)))
 
 
-def kvpr_verify_step(target_logits, draft_logits, logits_type, ld_target, ld_draft, vocab, tokens, row_start, seq_len, n_requests, n_rows,
+def kvpr_verify_step(target_logits, draft_logits, logits_type, ld_target, ld_draft, vocab, tokens, row_start, seq_len, certain, n_requests, n_rows,
                      temperature, u_accept, u_sample, len_in, len_out, kept, out_tokens, ws_dev, ws_bytes, stream=None):
     dtype = _FLOATS.get(logits_type)
     _typed(target_logits, dtype, "target_logits")
     _typed(draft_logits, dtype, "draft_logits")
-    d, target, draft, tok, start, seq, temp, ua, us, li, lo, kp, out, ws = _addresses(
-        target_logits, draft_logits, tokens, row_start, seq_len, temperature, u_accept, u_sample, len_in, len_out, kept, out_tokens, ws_dev)
-    _check(lib.kvpr_verify_step(target, draft, logits_type, ld_target, ld_draft, vocab, tok, start, seq, n_requests, n_rows, temp, ua, us, li, lo,
+    d, target, draft, tok, start, seq, sure, temp, ua, us, li, lo, kp, out, ws = _addresses(
+        target_logits, draft_logits, tokens, row_start, seq_len, certain, temperature, u_accept, u_sample, len_in, len_out, kept, out_tokens, ws_dev)
+    _check(lib.kvpr_verify_step(target, draft, logits_type, ld_target, ld_draft, vocab, tok, start, seq, sure, n_requests, n_rows, temp, ua, us, li, lo,
                                 kp, out, ws, ws_bytes, _current(d, stream)))

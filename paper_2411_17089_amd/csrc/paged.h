@@ -54,7 +54,8 @@ int launch_paged_attention(const PagedShape& s, const PagedAttention& a, void* w
 struct Verify {
     const void *target, *draft;
     int64_t ld_target, ld_draft;
-    const int32_t *tokens, *row_start, *seq_len, *len_in;       // seq_len null: no request was refused
+    const int32_t *tokens, *row_start, *len_in;
+    const int32_t *seq_len, *certain;           // null: no request was refused; one certain token each
     const float *temperature, *u_accept, *u_sample;
     int32_t *len_out, *kept, *out;
     int vocab, n, rows;

@@ -122,8 +122,8 @@ extern "C" size_t kvpr_verify_workspace_bytes(int n_requests, int n_rows, int vo
 }
 
 extern "C" int kvpr_verify_step(const void* target_logits, const void* draft_logits, int logits_type, int64_t ld_target, int64_t ld_draft, int vocab,
-                                const int32_t* tokens, const int32_t* row_start, const int32_t* seq_len, int n_requests, int n_rows,
-                                const float* temperature, const float* u_accept, const float* u_sample, const int32_t* len_in, int32_t* len_out,
+                                const int32_t* tokens, const int32_t* row_start, const int32_t* seq_len, const int32_t* certain, int n_requests,
+                                int n_rows, const float* temperature, const float* u_accept, const float* u_sample, const int32_t* len_in, int32_t* len_out,
                                 int32_t* kept, int32_t* out_tokens, void* ws, size_t ws_bytes, void* stream) {
     if (int rc = check_verify(n_requests, n_rows, vocab)) return rc;
     if (logits_type != KVPR_F16 && logits_type != KVPR_F32) return fail(KVPR_E_INVAL, "logits_type must be KVPR_F16 or KVPR_F32");
@@ -135,7 +135,7 @@ extern "C" int kvpr_verify_step(const void* target_logits, const void* draft_log
     if (((uintptr_t)target_logits | (uintptr_t)draft_logits) & elem || !aligned16(ws)) return fail(KVPR_E_INVAL, "logits or ws not aligned");
     const size_t need = kvpr::verify_workspace_bytes(n_requests, n_rows, vocab);
     if (!ws || ws_bytes < need) return fail(KVPR_E_INVAL, "the workspace must hold %zu bytes", need);
-    const kvpr::Verify v{target_logits, draft_logits, ld_target, ld_draft, tokens, row_start, seq_len, len_in, temperature, u_accept, u_sample, len_out, kept,
+    const kvpr::Verify v{target_logits, draft_logits, ld_target, ld_draft, tokens, row_start, len_in, seq_len, certain, temperature, u_accept, u_sample, len_out, kept,
                          out_tokens, vocab, n_requests, n_rows, logits_type == KVPR_F16};
     return kvpr::launch_verify(v, ws, (hipStream_t)stream);
 }
@@ -144,6 +144,6 @@ extern "C" int kvpr_verify_drafts(const void* target_logits, const void* draft_l
                                   const int32_t* tokens, const int32_t* row_start, int n_requests, int n_rows, const float* temperature,
                                   const float* u_accept, const float* u_sample, const int32_t* len_in, int32_t* len_out, int32_t* kept,
                                   int32_t* out_tokens, void* ws, size_t ws_bytes, void* stream) {
-    return kvpr_verify_step(target_logits, draft_logits, logits_type, ld_target, ld_draft, vocab, tokens, row_start, nullptr, n_requests, n_rows, temperature,
-                            u_accept, u_sample, len_in, len_out, kept, out_tokens, ws, ws_bytes, stream);
+    return kvpr_verify_step(target_logits, draft_logits, logits_type, ld_target, ld_draft, vocab, tokens, row_start, nullptr, nullptr, n_requests, n_rows,
+                            temperature, u_accept, u_sample, len_in, len_out, kept, out_tokens, ws, ws_bytes, stream);
 }

@@ -1,5 +1,5 @@
 // Verification of drafted tokens against the target's probabilities, from given random numbers (formulas at kvpr_verify_drafts; kvpr_verify_step is the
-// same behind a plan that may have refused requests).
+// same behind a plan that may have refused requests, and with prompt chunks).
 //
 // Three launches over chunks of the vocabulary, since the order of a request's steps leaves one workgroup per request otherwise
 // (five rows of 50272: 226 us in one workgroup):
@@ -125,6 +125,11 @@ template <> struct Eight<_Float16> {
     __device__ float at(int i) const { return (float)a[i]; }
 };
 
+// the last certain row of a request with rows first .. end - 1: those in front of it are followed by a token that needs no verification
+__device__ __forceinline__ int last_certain(const Verify& v, int r, int first, int end) {
+    return v.certain ? first + min(max(v.certain[r], 1), end - first) - 1 : first;
+}
+
 // E elements a thread, in pieces of 8
 template <class T, int E>
 __global__ __launch_bounds__(THREADS) void verify_stats(const VerifyArgs a) {
@@ -149,16 +154,20 @@ __global__ __launch_bounds__(THREADS) void verify_stats(const VerifyArgs a) {
             if (i + 8 <= n) x[j].load(from + i);
         }
     };
-    // a row of the target is asked for meanwhile; one of the draft only once it is known to be no request's first, which need not be there
-    if (!side) ask();
+    // a row of the target is asked for meanwhile; one of the draft only once it is known to be a draft's: the others need not be there.  With
+    // prompts most rows of the target are not needed either
+    const bool early = !side && !v.certain;
+    if (early) ask();
     __syncthreads();
     int owner = 0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) owner += counts[w];
     const int first = v.row_start[owner];
-    if (row >= v.row_start[owner + 1] || row < first || (side && row == first)) return;
-    if (v.seq_len && v.seq_len[owner] <= 0) return;
-    if (side) ask();
+    const int end = min(v.row_start[owner + 1], v.rows);
+    if (row >= end || row < first || (v.seq_len && v.seq_len[owner] <= 0)) return;
+    const int from_row = last_certain(v, owner, max(first, 0), end);
+    if (row < from_row || (side && row == from_row)) return;
+    if (!early) ask();
     const double inv_t = inverse(v.temperature[owner]);
     // the elements that are no whole piece of 8: at most 7, one a thread
     const int tail = n & ~7;
@@ -282,7 +291,7 @@ __device__ __forceinline__ int shares_of_chunk(const Shares<T>& s, int chunk, in
     return i;
 }
 
-// One workgroup per request: its rows joined, a wave per row and eight rows at a time, up to the first draft that does not stand
+// One workgroup per request: its rows from the last certain one on joined, a wave per row and eight rows at a time, up to the first draft that does not stand
 // (five rows of 50272: 5.4 us, with four at a time 6.7; 64 requests of 32000: 6.2 and 9.1).
 constexpr int DECIDE_WAVES = 8;
 template <class T>
@@ -303,7 +312,7 @@ __global__ __launch_bounds__(DECIDE_WAVES * 64) void verify_decide(const VerifyA
         for (int i = first + tid; i < end; i += DECIDE_WAVES * 64) v.out[i] = -1;
         return;
     }
-    for (int at = first;; at += DECIDE_WAVES) {
+    for (int at = last_certain(v, r, first, end);; at += DECIDE_WAVES) {
         if (tid == 0) stop = end;
         __syncthreads();
         const int row = at + wave;

@@ -62,7 +62,8 @@ class Server:
         u = self.u.index_select(0, self.step_no)[0]
         self.ua, self.us = u[:ROWS].contiguous(), u[ROWS:].contiguous()
         self.draft_logits.copy_(self.guesses.index_select(0, self.step_no)[0])
-        k.kvpr_verify_step(self.logits, self.draft_logits, k.KVPR_F32, VOCAB, VOCAB, VOCAB, self.tokens, self.row_start, self.seq_len, N, ROWS, self.temperature,
+        k.kvpr_verify_step(self.logits, self.draft_logits, k.KVPR_F32, VOCAB, VOCAB, VOCAB, self.tokens, self.row_start, self.seq_len, None, N, ROWS,
+                           self.temperature,
                            self.ua, self.us, self.base, self.base, self.kept, self.out, self.ws_v, self.ws_v.numel())
 
     def advance(self):
@@ -178,7 +179,7 @@ def test_verification_of_refused_requests(k, dtype, with_draft):
         got_kept, out, after = i32([-7] * n), i32([-7] * rows), i32(lens)
         ws = torch.full((k.kvpr_verify_workspace_bytes(n, rows, vocab),), 0xFF, dtype=torch.uint8, device="cuda")
         k.kvpr_verify_step(up(target), up(draft), k.KVPR_F16 if dtype == np.float16 else k.KVPR_F32, vocab, vocab, vocab, i32(tokens), i32(start),
-                           None if seq is None else i32(seq), n, rows, up(temperature), up(ua), up(us), after, after, got_kept, out, ws, ws.numel())
+                           None if seq is None else i32(seq), None, n, rows, up(temperature), up(ua), up(us), after, after, got_kept, out, ws, ws.numel())
         torch.cuda.synchronize()
         assert got_kept.tolist() == kept and out.tolist() == want
         assert after.tolist() == (lens + np.array(kept)).tolist()

@@ -22,9 +22,21 @@ def test_nothing_of_a_refused_request_is_kept():
     assert po.verify(*args) == ([2] * 6, [3, 3])                        # without the lengths it cannot know
 
 
+def test_certain_tokens_stand_by_hand():
+    logits = np.zeros((6, 4))
+    logits[:, 2] = 5                                                    # the model would always say 2
+    tokens, start = [0, 1, 3, 0, 2, 1], [0, 3, 6]
+    args = (logits, logits, tokens, start, [0.0, 0.0], [0.0] * 6, [0.5, 0.5], 6)
+    # a chunk of three prompt tokens; two certain tokens and a draft that the model does not bear out
+    assert po.verify(*args, certain=[3, 2]) == ([1, 3, 2, 2, 2, -1], [3, 2])
+    assert po.verify(*args, certain=[0, 9]) == ([2, -1, -1, 2, 1, 2], [1, 3])
+    assert po.verify(*args) == ([2, -1, -1, 2, 2, -1], [1, 2])
+    assert po.verify(*args, seq_len=[0, 9], certain=[3, 3]) == ([-1, -1, -1, 2, 1, 2], [0, 3])
+
+
 def _call(k, **change):
     P = 1 << 20                                                       # an aligned address that no refused call touches
-    args = dict(target_logits=P, draft_logits=P, logits_type=k.KVPR_F32, ld_target=100, ld_draft=100, vocab=100, tokens=P, row_start=P, seq_len=P,
+    args = dict(target_logits=P, draft_logits=P, logits_type=k.KVPR_F32, ld_target=100, ld_draft=100, vocab=100, tokens=P, row_start=P, seq_len=P, certain=P,
                 n_requests=1, n_rows=1, temperature=P, u_accept=P, u_sample=P, len_in=P, len_out=P, kept=P, out_tokens=P, ws_dev=P, ws_bytes=1 << 40)
     return k.kvpr_verify_step(**{**args, **change}, stream=0)
 
@@ -46,8 +58,9 @@ def test_bad_arguments(k, monkeypatch, name, value, code):
 def test_tensors_of_the_wrong_kind(k, monkeypatch):
     import torch
     monkeypatch.setattr(k.binding.torch.cuda, "current_device", lambda: 0)
-    with pytest.raises(ValueError, match="current device"):
-        _call(k, seq_len=torch.zeros(16, dtype=torch.int32))
+    for name in ("seq_len", "certain"):
+        with pytest.raises(ValueError, match="current device"):
+            _call(k, **{name: torch.zeros(16, dtype=torch.int32)})
     for name in ("target_logits", "draft_logits"):
         with pytest.raises(TypeError, match="must be torch.float32"):
             _call(k, **{name: torch.zeros(16, dtype=torch.float16)})
