@@ -11,6 +11,7 @@
 // their bytes over between its lanes and stores whole words; other rows store bytes.
 #include "int4_codec.h"
 #include "paged.h"
+#include <algorithm>
 
 namespace kvpr {
 namespace {
@@ -249,8 +250,12 @@ __global__ __launch_bounds__(WAVES * 64) void paged_read_kernel(PagedShape s, co
 
 }  // namespace
 
-int launch_paged_append(const PagedShape& s, const void* qkv, int64_t ld, const int32_t* slots, const int32_t* positions, int rows,
-                        const void* rope, int n_pos, void* q_out, int64_t ldq, void* pages, hipStream_t st) {
+// Rows of one launch: a dimension of a grid holds less than 2^32 threads, which 2^28 rows of an append and 2^26 of a read would pass.  A multiple of
+// the rows of a workgroup; a quad of positions that lies across the border is stored byte by byte.
+constexpr int MOST_AT_ONCE = 1 << 24;
+
+static int append_rows(const PagedShape& s, const void* qkv, int64_t ld, const int32_t* slots, const int32_t* positions, int rows,
+                       const void* rope, int n_pos, void* q_out, int64_t ldq, void* pages, hipStream_t st) {
     const int units = ((q_out ? s.heads : 0) + 2 * s.kv_heads) * s.d / 128 + 1;      // of a wave: one head, two of 64 columns
     const int64_t quads = ((int64_t)rows + 3) / 4;
     // Eight heads a wave, whose slots and angles are then looked up once; one where that would leave the GPU's 1024 SIMDs without two waves each
@@ -266,7 +271,17 @@ int launch_paged_append(const PagedShape& s, const void* qkv, int64_t ld, const 
     return many ? launch(paged_append_kernel<64, 8>, 8) : launch(paged_append_kernel<64, 1>, 1);
 }
 
-int launch_paged_read(const PagedShape& s, const void* pages, const int32_t* slots, int rows, void* kv, int64_t ld, hipStream_t st) {
+int launch_paged_append(const PagedShape& s, const void* qkv, int64_t ld, const int32_t* slots, const int32_t* positions, int rows,
+                        const void* rope, int n_pos, void* q_out, int64_t ldq, void* pages, hipStream_t st) {
+    for (int64_t r = 0; r < rows; r += MOST_AT_ONCE) {
+        const int rc = append_rows(s, (const _Float16*)qkv + r * ld, ld, slots + r, positions ? positions + r : nullptr, (int)std::min<int64_t>(rows - r, MOST_AT_ONCE),
+                                   rope, n_pos, q_out ? (_Float16*)q_out + r * ldq : nullptr, ldq, pages, st);
+        if (rc) return rc;
+    }
+    return KVPR_OK;
+}
+
+static int read_rows(const PagedShape& s, const void* pages, const int32_t* slots, int rows, void* kv, int64_t ld, hipStream_t st) {
     const int units = (2 * s.kv_heads * s.d + 127) / 128;
     const int64_t quads = ((int64_t)rows + 3) / 4;
     const int each = quads * units >= 8 * 2048 ? 4 : 1;      // as above
@@ -274,6 +289,12 @@ int launch_paged_read(const PagedShape& s, const void* pages, const int32_t* slo
     auto kern = s.d == 128 ? (each == 4 ? paged_read_kernel<128, 4> : paged_read_kernel<128, 1>) : each == 4 ? paged_read_kernel<64, 4> : paged_read_kernel<64, 1>;
     hipLaunchKernelGGL(kern, grid, dim3(WAVES * 64), 0, st, s, (const uint8_t*)pages, slots, rows, (_Float16*)kv, ld);
     KVPR_HIP(hipGetLastError());
+    return KVPR_OK;
+}
+
+int launch_paged_read(const PagedShape& s, const void* pages, const int32_t* slots, int rows, void* kv, int64_t ld, hipStream_t st) {
+    for (int64_t r = 0; r < rows; r += MOST_AT_ONCE)
+        if (const int rc = read_rows(s, pages, slots + r, (int)std::min<int64_t>(rows - r, MOST_AT_ONCE), (_Float16*)kv + r * ld, ld, st)) return rc;
     return KVPR_OK;
 }
 
