@@ -250,13 +250,13 @@ __global__ __launch_bounds__(WAVES * 64) void paged_read_kernel(PagedShape s, co
 
 }  // namespace
 
-// Rows of one launch: a dimension of a grid holds less than 2^32 threads, which 2^28 rows of an append and 2^26 of a read would pass.  A multiple of
-// the rows of a workgroup; a quad of positions that lies across the border is stored byte by byte.
+// Rows of one launch: a dimension of a grid holds less than 2^32 threads, which 2^28 rows of an append and 2^26 of a read would pass (unreported: the read
+// left nearly all rows as they were).  A multiple of the rows of a workgroup; a quad of positions that lies across the border is stored byte by byte.
 constexpr int MOST_AT_ONCE = 1 << 24;
 
 static int append_rows(const PagedShape& s, const void* qkv, int64_t ld, const int32_t* slots, const int32_t* positions, int rows,
                        const void* rope, int n_pos, void* q_out, int64_t ldq, void* pages, hipStream_t st) {
-    const int units = ((q_out ? s.heads : 0) + 2 * s.kv_heads) * s.d / 128 + 1;      // of a wave: one head, two of 64 columns
+    const int units = (((q_out ? s.heads : 0) + 2 * s.kv_heads) * s.d + 127) / 128;      // of a wave: one head, two of 64 columns
     const int64_t quads = ((int64_t)rows + 3) / 4;
     // Eight heads a wave, whose slots and angles are then looked up once; one where that would leave the GPU's 1024 SIMDs without two waves each
     const bool many = quads * units >= 8 * 2048;
