@@ -63,9 +63,12 @@ class KvprError(RuntimeError):
         self.code = code
 
 
-if not os.path.exists(LIB_PATH):
-    raise ImportError(f"{LIB_PATH} not found: build it with `python paper_2411_17089_amd/build.py` "
+for _path in (LIB_PATH, os.path.join(_HERE, "_tensor_args.so")):
+    if not os.path.exists(_path):
+        raise ImportError(f"{_path} not found: build it with `python paper_2411_17089_amd/build.py` "
                       "(there is no CPU fallback)")
+from ._tensor_args import addresses as _addresses  # noqa: E402
+
 lib = C.CDLL(LIB_PATH)
 
 _vp, _i, _i64, _sz = C.c_void_p, C.c_int, C.c_int64, C.c_size_t
@@ -406,36 +409,17 @@ def kvpr_decode_attention_mixed(q_dev, kv16_dev, kvq_dev, z_dev, ws_dev, S, spli
 
 
 # ---- ragged batches over a paged 4-bit cache ----
-# Device arguments must be tensors on the current device (a host address in a kernel's hands would end the process), the
-# floating ones of the stated type.  A step of a small batch is a few microseconds on the GPU, so they are looked over without a Python
-# call for each: that took 0.9 us an argument, more than the rest of a plan.
+# Device arguments must be tensors on the current device (a host address in a kernel's hands would end the process) of the stated type: int32, float32,
+# or what the call's own type argument says.  Those that the call has no stride for must be contiguous.  Raw addresses are passed on as they are.
 
-_data_ptr, _get_device = torch.Tensor.data_ptr, torch.Tensor.get_device
-_FLOATS = {KVPR_F16: torch.float16, KVPR_F32: torch.float32}
-
-
-def _addresses(*tensors):
-    """Device addresses of tensors, None or ints, and the current device's index in front."""
-    d = torch.cuda.current_device()
-    try:
-        if set(map(_get_device, tensors)) == {d}:
-            return [d, *map(_data_ptr, tensors)]
-    except TypeError:                               # not tensors alone
-        pass
-    out = [d]
-    for i, t in enumerate(tensors):
-        if t is None or isinstance(t, int):
-            out.append(t)
-        elif t.get_device() != d:
-            raise ValueError(f"tensor {i + 1} of the call must be on the current device cuda:{d}, got {t.device}")
-        else:
-            out.append(t.data_ptr())
-    return out
-
-
-def _typed(t, dtype, name):
-    if dtype is not None and getattr(t, "dtype", dtype) is not dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+_ROWS = {KVPR_F16: "h", KVPR_F32: "s"}             # kind of a row-wise argument; other numbers are the library's to refuse
+_PLAN_NAMES = ("base_len", "new_len", "block_table", "held_in", "held_out", "free_pages", "free_count_in", "free_count_out", "row_start", "seq_len", "slots",
+               "positions", "refused")
+_APPEND_NAMES = ("qkv_dev", "slots", "positions", "rope_table", "q_out", "pages")
+_READ_NAMES = ("pages", "slots", "kv_dev")
+_ATTENTION_NAMES = ("q_dev", "pages", "block_table", "row_start", "seq_len", "z_dev", "ws_dev")
+_VERIFY_NAMES = ("target_logits", "draft_logits", "tokens", "row_start", "temperature", "u_accept", "u_sample", "len_in", "len_out", "kept", "out_tokens", "ws_dev")
+_VERIFY_STEP_NAMES = _VERIFY_NAMES[:4] + ("seq_len", "certain") + _VERIFY_NAMES[4:]
 
 
 def _current(device, stream):
@@ -452,23 +436,23 @@ def kvpr_page_bytes(desc) -> int:
 
 def kvpr_paged_plan(desc, base_len, new_len, n_requests, block_table, held_in, held_out, free_pages, free_count_in, free_count_out,
                     max_rows, row_start, seq_len, slots, positions, refused, stream=None):
-    d, base, new, table, hi, ho, free, ci, co, start, seq, slot, pos, ref = _addresses(
+    d = torch.cuda.current_device()
+    base, new, table, hi, ho, free, ci, co, start, seq, slot, pos, ref = _addresses(
+        d, "iiiiiiiiiiiii", _PLAN_NAMES,
         base_len, new_len, block_table, held_in, held_out, free_pages, free_count_in, free_count_out, row_start, seq_len, slots, positions, refused)
     _check(lib.kvpr_paged_plan(C.byref(desc), base, new, n_requests, table, hi, ho, free, ci, co, max_rows, start, seq, slot, pos, ref,
                                _current(d, stream)))
 
 
 def kvpr_paged_append(desc, qkv_dev, ld, slots, positions, n_rows, rope_table, n_pos, q_out, ldq, pages, stream=None):
-    _typed(qkv_dev, torch.float16, "qkv_dev")
-    _typed(q_out, torch.float16, "q_out")
-    _typed(rope_table, torch.float32, "rope_table")
-    d, qkv, slot, pos, rope, q, pool = _addresses(qkv_dev, slots, positions, rope_table, q_out, pages)
+    d = torch.cuda.current_device()
+    qkv, slot, pos, rope, q, pool = _addresses(d, "hiifhb", _APPEND_NAMES, qkv_dev, slots, positions, rope_table, q_out, pages)
     _check(lib.kvpr_paged_append(C.byref(desc), qkv, ld, slot, pos, n_rows, rope, n_pos, q, ldq, pool, _current(d, stream)))
 
 
 def kvpr_paged_read(desc, pages, slots, n_rows, kv_dev, ld, stream=None):
-    _typed(kv_dev, torch.float16, "kv_dev")
-    d, pool, slot, kv = _addresses(pages, slots, kv_dev)
+    d = torch.cuda.current_device()
+    pool, slot, kv = _addresses(d, "bih", _READ_NAMES, pages, slots, kv_dev)
     _check(lib.kvpr_paged_read(C.byref(desc), pool, slot, n_rows, kv, ld, _current(d, stream)))
 
 
@@ -478,9 +462,9 @@ def kvpr_paged_attention_workspace_bytes(desc, n_requests, n_rows, max_new, max_
 
 def kvpr_paged_attention(desc, q_dev, q_type, ldq, pages, block_table, row_start, seq_len, n_requests, n_rows, max_new, max_len, z_dev, ldz,
                          ws_dev, ws_bytes, stream=None):
-    _typed(q_dev, _FLOATS.get(q_type), "q_dev")
-    _typed(z_dev, torch.float16, "z_dev")
-    d, q, pool, table, start, seq, z, ws = _addresses(q_dev, pages, block_table, row_start, seq_len, z_dev, ws_dev)
+    d = torch.cuda.current_device()
+    q, pool, table, start, seq, z, ws = _addresses(
+        d, _ROWS.get(q_type, "r") + "biiihb", _ATTENTION_NAMES, q_dev, pages, block_table, row_start, seq_len, z_dev, ws_dev)
     _check(lib.kvpr_paged_attention(C.byref(desc), q, q_type, ldq, pool, table, start, seq, n_requests, n_rows, max_new, max_len, z, ldz, ws,
                                     ws_bytes, _current(d, stream)))
 
@@ -491,10 +475,9 @@ def kvpr_verify_workspace_bytes(n_requests, n_rows, vocab) -> int:
 
 def kvpr_verify_drafts(target_logits, draft_logits, logits_type, ld_target, ld_draft, vocab, tokens, row_start, n_requests, n_rows, temperature,
                        u_accept, u_sample, len_in, len_out, kept, out_tokens, ws_dev, ws_bytes, stream=None):
-    dtype = _FLOATS.get(logits_type)
-    _typed(target_logits, dtype, "target_logits")
-    _typed(draft_logits, dtype, "draft_logits")
-    d, target, draft, tok, start, temp, ua, us, li, lo, kp, out, ws = _addresses(
+    d = torch.cuda.current_device()
+    target, draft, tok, start, temp, ua, us, li, lo, kp, out, ws = _addresses(
+        d, 2 * _ROWS.get(logits_type, "r") + "iifffiiiib", _VERIFY_NAMES,
         target_logits, draft_logits, tokens, row_start, temperature, u_accept, u_sample, len_in, len_out, kept, out_tokens, ws_dev)
     _check(lib.kvpr_verify_drafts(target, draft, logits_type, ld_target, ld_draft, vocab, tok, start, n_requests, n_rows, temp, ua, us, li, lo,
                                   kp, out, ws, ws_bytes, _current(d, stream)))
@@ -502,10 +485,9 @@ def kvpr_verify_drafts(target_logits, draft_logits, logits_type, ld_target, ld_d
 
 def kvpr_verify_step(target_logits, draft_logits, logits_type, ld_target, ld_draft, vocab, tokens, row_start, seq_len, certain, n_requests, n_rows,
                      temperature, u_accept, u_sample, len_in, len_out, kept, out_tokens, ws_dev, ws_bytes, stream=None):
-    dtype = _FLOATS.get(logits_type)
-    _typed(target_logits, dtype, "target_logits")
-    _typed(draft_logits, dtype, "draft_logits")
-    d, target, draft, tok, start, seq, sure, temp, ua, us, li, lo, kp, out, ws = _addresses(
+    d = torch.cuda.current_device()
+    target, draft, tok, start, seq, sure, temp, ua, us, li, lo, kp, out, ws = _addresses(
+        d, 2 * _ROWS.get(logits_type, "r") + "iiiifffiiiib", _VERIFY_STEP_NAMES,
         target_logits, draft_logits, tokens, row_start, seq_len, certain, temperature, u_accept, u_sample, len_in, len_out, kept, out_tokens, ws_dev)
     _check(lib.kvpr_verify_step(target, draft, logits_type, ld_target, ld_draft, vocab, tok, start, seq, sure, n_requests, n_rows, temp, ua, us, li, lo,
                                 kp, out, ws, ws_bytes, _current(d, stream)))
