@@ -303,7 +303,7 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
         int seen[MT];
         bool real[MT];
         Half8 q[MT][W];
-        float qs[MT][NG], to_log2[MT];
+        float qs[MT][NG], score_unit[MT], to_log2[MT];      // unit of the scores, and that of the weights: smaller where scores are very large
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             int token, head;
@@ -328,10 +328,11 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
                 for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(x[st][e]));
             }
             big = across_rows(big, max_of);
-            // exponent of the largest element; of 0 and of infinite or NaN rows whatever
-            const int ex = min(max((int)(__float_as_uint(big) >> 23) - 127, -100), 100);
+            // exponent of the largest element (of 0 whatever); infinite and NaN rows become NaN
+            const int ex = max((int)(__float_as_uint(big) >> 23) - 127, -100);
             const float up = __uint_as_float((uint32_t)(127 + 10 - ex) << 23);
-            to_log2[mt] = a.scale_log2 * __uint_as_float((uint32_t)(127 + 24 - 10 + ex) << 23);
+            // beyond 2^85 the unit stays, so that no score overflows: any two that float32 tells apart are 2^30 and more apart there anyway
+            score_unit[mt] = to_log2[mt] = a.scale_log2 * __uint_as_float((uint32_t)(127 + 24 - 10 + min(ex, 85)) << 23);
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
                 float t = 0.f;
@@ -357,11 +358,11 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
             }
         }
 
-        float ref[MT], l[MT];
+        float ref[MT], off[MT], l[MT];                      // off: the score that ref was set from
         float4v acc[MT][NT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            ref[mt] = LOWEST;
+            ref[mt] = off[mt] = LOWEST;
             l[mt] = 0.f;
 #pragma unroll
             for (int t = 0; t < NT; ++t) acc[mt][t] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -470,8 +471,15 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
 #pragma unroll
                 for (int j = 1; j < 8; ++j) top = fmaxf(top, sc[mt][j >> 2][j & 3]);
                 if (__any(fmaf(top, to_log2[mt], -ref[mt]) > 15.f)) {
-                    const float now = fmaxf(ref[mt], across_rows(top, max_of) * to_log2[mt] - 6.f);
-                    const float keep = exp2f(ref[mt] - now);
+                    // Weights are exact to ref as it is rounded, which beyond 2^27 would carry them out of float16.  Scores of 2^26 and more are
+                    // known to no better than 16 anyway, so their row's differences are counted in units of a power of two that brings them to 2^25 .. 2^26
+                    const float was = off[mt];
+                    off[mt] = fmaxf(was, across_rows(top, max_of));
+                    const int over = max((int)(__float_as_uint(fabsf(off[mt] * score_unit[mt])) >> 23) - (127 + 25), 0);
+                    const bool fine = over == 0 && to_log2[mt] == score_unit[mt];
+                    to_log2[mt] = score_unit[mt] * __uint_as_float((uint32_t)(127 - over) << 23);
+                    const float now = off[mt] == LOWEST ? LOWEST : off[mt] * to_log2[mt] - 6.f;
+                    const float keep = exp2f(fine ? ref[mt] - now : (was - off[mt]) * score_unit[mt]);
                     ref[mt] = now;
                     l[mt] *= keep;
 #pragma unroll
@@ -561,7 +569,7 @@ __global__ __launch_bounds__(NW * 64, MT == 1 ? 3 : 2) void paged_attention_kern
             if (mt * 16 >= live_rows) break;
             int token, head;
             const bool real = place(mt, token, head);
-            float lsum = l[mt], top = ref[mt];
+            float lsum = l[mt], top = to_log2[mt] == score_unit[mt] || off[mt] == LOWEST ? ref[mt] : off[mt] * score_unit[mt] - 6.f;
             // columns 64 gr + 16 g + 4 p .. + 3 of one row from acc over (w, h)
             auto put = [&](int p, int gr, const float (&what)[4]) {
                 if (!real) return;
