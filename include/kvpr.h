@@ -498,6 +498,7 @@ int kvpr_paged_plan(const kvpr_paged_desc* desc, const int32_t* base_len, const 
  * With rope_table (device copy of kvpr_rope_table's [n_pos, head_dim/2, 2]) k is rotated first, and q rotated into q_out (float16, row
  * stride ldq; null: not wanted; q itself, with ldq = ld, is allowed), both by the row's position, evaluated in 64 bits and rounded to
  * float16 once; a row whose position lies outside [0, n_pos) is left out.  Without rope_table positions may be null and q_out must be.
+ * A NaN is packed as the smallest number of its group (a group of nothing but NaN stays NaN); a group with an infinity gives no finite value back.
  * ld, ldq % 8 == 0; qkv, q_out, pages 16-byte aligned.  Two rows must not name the same slot. */
 int kvpr_paged_append(const kvpr_paged_desc* desc, const void* qkv, int64_t ld, const int32_t* slots, const int32_t* positions, int n_rows,
                       const void* rope_table, int n_pos, void* q_out, int64_t ldq, void* pages, void* stream);
