@@ -510,10 +510,12 @@ int kvpr_paged_read(const kvpr_paged_desc* desc, const void* pages, const int32_
  * included), row i of request r sees positions [0, seq_len[r] - m + i + 1): z = softmax(q k^T / sqrt(head_dim)) v in float16, row stride ldz.
  * A row that sees nothing gives 0.  k is code * scale + minimum, v that rounded to float16 as kvpr_dequant_int4 gives it.  Positions whose table entry lies
  * outside the pool, or behind table_width entries, take no part.
- * Values that are not finite (scales, minima, or 15 scale + minimum beyond float16's range) leave rows that do not see their position as they are; rows that do
- * are not finite in the columns of those values, and may be NaN in their other columns too.
+ * Values that are not finite leave rows that do not see their position as they are; rows that do are not finite in the columns of those values, and may be NaN in
+ * their other columns too.  A position counts as such a one where its scale or minimum is not finite, or 15 scale + minimum passes float16's range, a code of 15 in it or
+ * not (kvpr_paged_append leaves one in every group).  Scores may be of any finite size; what float32 cannot tell apart counts as equal or nearly so.
  * q: KVPR_F16 or KVPR_F32, row stride ldq (elements).  max_new and max_len: how many new tokens and positions a request has at most,
- * as far as the host knows; they size the launch and the workspace, and results are right for requests beyond them too.
+ * as far as the host knows; they size the launch and the workspace and choose the kernel, and results are right for requests beyond them too (a batch with a
+ * prompt chunk beside many long requests with a row each is faster with max_new = 1).
  * ldq, ldz % 8 == 0; q, pages, z, ws 16-byte aligned; ws needs kvpr_paged_attention_workspace_bytes of the same arguments. */
 size_t kvpr_paged_attention_workspace_bytes(const kvpr_paged_desc* desc, int n_requests, int n_rows, int max_new, int max_len);
 int kvpr_paged_attention(const kvpr_paged_desc* desc, const void* q, int q_type, int64_t ldq, const void* pages, const int32_t* block_table,
@@ -526,7 +528,7 @@ int kvpr_paged_attention(const kvpr_paged_desc* desc, const void* q, int q_type,
  *   p = softmax(target row i / T), q = softmax(draft row i + 1 / T), T = temperature[r];
  *   draft x = tokens[row i + 1] stands if u_accept[row i + 1] q(x) < p(x); the first that does not ends the run;
  *   the next token is the first v with sum_{w <= v} s(w) > u_sample[r] sum_w s(w), s = max(p - q, 0) of the row that was rejected (p where that
- *   leaves nothing), s = p behind the last draft.  Shares and sums are evaluated in 64 bits.  u in [0, 1).
+ *   leaves nothing), s = p behind the last draft.  Shares are good to 2 10^-12 of their size, their sums are held in 64 bits.  u in [0, 1).
  * T above 10^30 counts as 10^30.  T <= 0 (or NaN): greedy, a draft stands if it is the row's largest logit (lowest index on ties), and the next token is the largest one.
  * Out: out_tokens of a request's rows: the drafts that stand, the next token, -1 for the rest; kept[r] = rows of the cache that stay = tokens gained
  * (0 for a request without rows); len_out[r] = len_in[r] + kept[r] (both null: not wanted; the same array is allowed): with len_in = base_len, the next plan's base_len.

@@ -10,14 +10,16 @@
 //     exactly: unpacking is a mask.  The factor 16 of the odd columns is taken out of q; the affine map is taken out of the
 //     sum, k . q = scale (code . q) + minimum sum(q), per group of 64 columns, in float32;
 //   - values are unpacked to float16, as kvpr_dequant_int4 gives them: (1024 + code) - 1024 exactly, then one fused
-//     multiplication and addition;
+//     multiplication and addition.  That rounding is the library's definition of a stored value (whatever reads the cache sees the same
+//     numbers), and the matrix instruction's operand; against values that are not rounded it makes the error 2.8 10^-4 of the result's size where
+//     the result's own rounding gives 2.1;
 //   - q is scaled by a power of two per row to a largest element of 2^10 .. 2^11; float32 q is brought as the sum of two
 //     float16 numbers (the rest below 2^-22 of the largest element);
 //   - weights are 2^(score - ref), brought to the product as the sum of two float16 numbers (one alone made the result's error 1.6
 //     times that of its own rounding), summed in float32.  ref is the largest score less 6 when it was
 //     last set and is set again only when a weight would pass 2^15: no reduction over lanes in the usual turn, and
 //     weights keep all bits down to 2^-20 of the largest, some to 2^-30.
-// What bounds it: long caches with one row a request the reading (32 x 1000 positions of 32 heads 36 us, 4.1 TB/s of packed rows); more
+// What bounds it: long caches with one row a request the reading (32 x 1000 positions of 32 heads 36 - 39 us, 3.8 - 4.1 TB/s of packed rows); more
 // rows a head the vector instructions between the products (unpacking 160 a turn and wave, 100 more for each tile of rows).
 // Work: a unit is (request, key/value head, tile of rows).  Few rows: the workgroup's waves share a tile and take turns of 32 positions in
 // turn, their sums meet in LDS; many rows: each wave has rows of its own.  The lengths are known on the device only.  Where the
@@ -692,7 +694,9 @@ Cut cut_of(const PagedShape& s, int n, int rows, int max_new, int max_len) {
     // A unit each for a workgroup, or equal runs of the work: runs cost a second launch and the sums in front of the first, 9 us in all, and
     // units that differ in length keep the GPU waiting for the longest.  us by units / by runs: 32 x 1000 positions, 32 heads 36 / 45; 64 x 1 to
     // 8192, 8 heads 104 / 52; 4 x 25000, 8 heads 276 / 64; two chunks of 1000 rows 215 / 270.  So units where they fill half of the GPU and none
-    // is longer than 16 turns, or where their rows are many, and where a unit has one turn.
+    // is longer than 16 turns, or where their rows are many, and where a unit has one turn.  The borders lie between these four.  max_new does not tell
+    // two chunks from one chunk beside many single rows, which are units too and then unequal ones: 2 chunks of 1000 and 30 rows over 20000 to 32000
+    // positions 960, where the chunks alone take 235 and the rows alone 179; with max_new given as 1, by runs of 16 rows, 480.
     c.direct = len <= step || (c.many_rows ? all >= resident / 2 : all >= resident / 2 && len <= 2048);
     if (c.direct) {
         c.groups = (int)std::min<int64_t>(units, 1 << 16);
