@@ -7,8 +7,8 @@
 //   verify_decide  a request's rows joined from their chunks, and the run of drafts that stand;
 //   verify_draw    of each chunk of the row behind them the sum of max(p - q, 0); the last workgroup of a request then finds the chunk in
 //                  which the random number falls, and the token in it.
-// The first reads everything once and is bound by its vector instructions, 38 to 42 a logit: at 4 cycles each and 2.4 GHz 31 of 34 us for 240 rows of 131071 in
-// float32 (whose bytes are 26), 13 of 19 for 380 rows of 32000 in float16.  The last reads one row of each model again, from the caches, and
+// The first reads everything once and is bound by its vector instructions, 38 a logit: at 4 cycles each and 2.4 GHz 31 of 34 us for 240 rows of 131071 in
+// float32 (whose bytes are 26), 13 of 19 for 400 rows of 32000 in float16.  The last reads one row of each model again, from the caches, and
 // is a chain of waits - loads, acknowledged stores, barriers - in which its waves spend 60 to 70 % of their time.
 // Shares, good to some 10^-12, and their sums are held in 64 bits: a uniform number falls between two of some 10^5 borders, and sums in 32 bits would
 // move those by more than a few per mille of the distance of the closer ones.  Partial sums are added in an order that depends on the sizes
@@ -26,7 +26,7 @@ constexpr int THREADS = 256, WAVES = THREADS / 64;
 __device__ __forceinline__ float logit(float v) { return v == v ? v : -INFINITY; }
 
 // 2^t for -1100 <= t <= 0, subnormal numbers among them: t = k + f with |f| <= 1/2 (adding 1.5 2^52 leaves k in the low word), the polynomial of degree 8 that meets 2^f
-// in the 9 Chebyshev points of that interval (off by 1.1 10^-12 at most, in turns above and below), ldexp: 14 of the about 40 vector instructions a
+// in the 9 Chebyshev points of that interval (off by 1.1 10^-12 at most, in turns above and below), ldexp: 14 of the 38 vector instructions a
 // logit, which bound the reading of many logits.  The library's exp and the steps around it are 40 by themselves.
 __device__ __forceinline__ double exp2_of(double t) {
     const double big = 6755399441055744.0, kd = t + big, f = t - (kd - big);
